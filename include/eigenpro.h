@@ -39,6 +39,13 @@ enum {
     EP_LAPLACIAN = 1   /* k(x,z) = exp(-|x-z| / bw)          (Appendix B)    */
 };
 
+/* Element types of the attention calls and of what a cache holds. */
+enum {
+    EP_BF16 = 0,
+    EP_FP16 = 1,
+    EP_E4M3 = 2        /* 8-bit values with a scale per row; caches only      */
+};
+
 typedef struct ep_ctx ep_ctx;
 
 /* Products of setup (Algorithm 1 initialisation; Sections 3 and 4). */
@@ -352,6 +359,167 @@ int ep_step_pass(ep_ctx* ctx, int64_t m, int* pass);
  * shader cycle counter to the 100 MHz constant counter). Blocking; about
  * 0.1 s. Either out-pointer may be NULL. Errors: EP_EDEVICE, EP_ENOMEM. */
 int ep_device_probe(double* mfma_f32_tflops, double* shader_clock_mhz);
+
+/*
+ * Attention: the kernel pass of ep_predict with the normalised exponential
+ * kernel, many small problems at once,
+ *
+ *   out_i = sum_j p_ij v_j,  p_ij = exp(scale q_i.k_j - lse_i),
+ *   lse_i = log sum_j exp(scale q_i.k_j)
+ *
+ * over the keys j that query i sees. These calls take no context: all work
+ * goes to the stream given, on the current device, asynchronously; they
+ * allocate nothing and can be captured into a graph. Results do not depend on
+ * the order in which workgroups run.
+ *
+ * Packed rows. A batch of sequences lies in one array, one after another:
+ * sequence b holds rows start[b] .. start[b+1] - 1 (device int32, batch + 1
+ * values, not decreasing). Rows behind the last sequence are neither read nor
+ * written. Values of start outside [0, tokens] are taken as the nearest
+ * inside.
+ *
+ * Heads. Query head h reads key head h / (heads / kv_heads).
+ *
+ * Mask. Query i of a sequence of n queries and m keys stands at position
+ * p = i + m - n. With causal it sees keys j <= p, with a window w > 0 (causal
+ * only) those with j > p - w; else it sees all. A query that sees nothing (p
+ * < 0, no keys) gets out = 0, lse = -infinity and no gradient. Keys and
+ * values must be finite: one that is not may reach any query of its sequence.
+ *
+ * Arithmetic. Scores, softmax statistics and sums are float32; probabilities
+ * (and, for gradients, p (dp - D)) are rounded to the element type for their
+ * products. EP_FP16 gradients: as everywhere in fp16, values below 2^-24
+ * vanish; scale the loss so that dout is of the order of one.
+ */
+
+/* Rows of heads: element (t, h, c) at data[t row + h head + c], 16-bit.
+ * data is 16-byte aligned, row and head are multiples of 8 (they may be
+ * strides into a wider array). */
+typedef struct ep_rows {
+    void* data;
+    int64_t row, head;
+} ep_rows;
+
+/* What the attention calls share. Bounds: 1 <= batch < 2^24; tokens_q,
+ * tokens_k >= 0 and < 2^30; heads a multiple of kv_heads, with group = heads /
+ * kv_heads: tokens_q group^2 < 2^32 and group <= 1024; kv_heads < 2^16; dim a
+ * multiple of 8, 8 .. 128; scale > 0 and finite; 0 <= window < 2^30. */
+typedef struct ep_attn {
+    int32_t type;               /* EP_BF16 or EP_FP16                          */
+    int32_t causal;             /* 0 or 1                                      */
+    int64_t batch, heads, kv_heads, dim;
+    int64_t tokens_q, tokens_k; /* rows of the packed arrays                   */
+    int64_t window;             /* 0: none                                     */
+    const int32_t* start_q;     /* device, batch + 1                           */
+    const int32_t* start_k;     /* device, batch + 1 (not ep_cache_attention)  */
+    float scale;
+} ep_attn;
+
+/*
+ * ep_attention — out and lse for packed queries, keys and values.
+ *   q    tokens_q x heads x dim.   k, v  tokens_k x kv_heads x dim.
+ *   out  as q; must not overlap the inputs.
+ *   lse  device float32 tokens_q x heads, or NULL.
+ * Errors: EP_EINVAL (the bounds of ep_attn and ep_rows, NULL), EP_EDEVICE.
+ */
+int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, ep_rows out, float* lse,
+                 void* hip_stream);
+
+/*
+ * ep_attention_backward — dq, dk, dv for a gradient dout of out. The
+ * probabilities are formed again from q, k and lse, so nothing of size n x m
+ * is stored.
+ *   out, lse  what ep_attention returned for the same a, q, k, v.
+ *   dq        as q.   dk, dv  as k, v: the sums over a group's heads. Every
+ *             row of every sequence is written (not added to). They must not
+ *             overlap the inputs or each other.
+ *   work      device, at least ep_attention_backward_bytes(a) bytes, 16-byte
+ *             aligned; holds nothing between calls. Calls that may overlap
+ *             need their own.
+ * Errors: EP_EINVAL (as ep_attention; work too small), EP_EDEVICE.
+ */
+int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, ep_rows k, ep_rows v,
+                          ep_rows out, const float* lse, ep_rows dq, ep_rows dk, ep_rows dv,
+                          void* work, int64_t work_bytes, void* hip_stream);
+/* Bytes of work for a call, or EP_EINVAL. */
+int64_t ep_attention_backward_bytes(const ep_attn* a);
+
+/*
+ * A paged cache of keys and values: pages of page_size tokens, tokens of
+ * kv_heads rows of dim values, contiguous; k and v alike. Sequence b's token j
+ * lies in page table[b cols + j / page_size].
+ *
+ * EP_E4M3: a row (one token, one head) is dim e4m3 numbers times its scale, the
+ * smallest power of two that brings its largest finite value within 448 (at
+ * least 2^-110, in fp16 2^-15; 1 for a row of zeros). Each value is rounded
+ * once, to nearest; what comes back is exact in the 16-bit type. Values above
+ * 1.875 times the type's largest power of two are stored as that; values that
+ * are not finite are stored as NaN.
+ */
+typedef struct ep_cache {
+    int32_t type;               /* what the pages hold: EP_BF16, EP_FP16, EP_E4M3 */
+    int64_t pages;              /* 1 .. 2^31 - 1                               */
+    int64_t page_size;          /* tokens, a power of two, at most 65536        */
+    int64_t kv_heads, dim;      /* as ep_attn                                  */
+    void* k;                    /* device, pages x page_size x kv_heads x dim,  */
+    void* v;                    /*   16-byte aligned                           */
+    float* k_scale;             /* EP_E4M3: device float32,                    */
+    float* v_scale;             /*   pages x page_size x kv_heads; else NULL   */
+} ep_cache;
+
+/* Which pages the sequences hold. cols * page_size < 2^30. A page number
+ * outside the cache, or a length outside [0, cols page_size], makes the
+ * results of its sequence unspecified and sets *err to 1; nothing outside the
+ * cache is read or written. */
+typedef struct ep_pages {
+    int64_t batch;
+    const int32_t* table;       /* device, batch x cols                        */
+    int64_t cols;
+    const int32_t* lengths;     /* device, batch: tokens of each sequence, new
+                                   ones included                               */
+    int32_t* err;               /* device, one value that the caller cleared,
+                                   or NULL                                     */
+} ep_pages;
+
+/*
+ * ep_cache_write — new tokens' keys and values into their pages, rounded to
+ * 8 bits if the cache holds EP_E4M3. Sequence b's new tokens are the packed
+ * rows start[b] .. start[b+1] - 1 and the last of its lengths[b] tokens.
+ *   type    of k and v, EP_BF16 or EP_FP16 (that of the cache unless EP_E4M3).
+ *   k, v    tokens x kv_heads x dim.   start  device, batch + 1.
+ * Tokens without a place (a bad page, a position below 0 or past the table)
+ * are not written and set *err. A page that two sequences share gets either's
+ * values where both write the same slot.
+ * Errors: EP_EINVAL, EP_EDEVICE.
+ */
+int ep_cache_write(const ep_cache* c, const ep_pages* p, int type, ep_rows k, ep_rows v,
+                   int64_t tokens, const int32_t* start, void* hip_stream);
+
+/*
+ * ep_cache_read — the cached rows back as packed rows of type EP_BF16 or
+ * EP_FP16: row start[b] + j gets token j of sequence b, for start[b+1] -
+ * start[b] tokens (at most lengths[b]; rows beyond are left as they were and
+ * set *err). Errors: EP_EINVAL, EP_EDEVICE.
+ */
+int ep_cache_read(const ep_cache* c, const ep_pages* p, int type, ep_rows k, ep_rows v,
+                  int64_t tokens, const int32_t* start, void* hip_stream);
+
+/*
+ * ep_cache_attention — ep_attention of new tokens' queries over the cache:
+ * sequence b's keys are its lengths[b] cached tokens (write the new ones
+ * first). From one token a sequence to whole prompts; a->start_k and
+ * a->tokens_k are not used. An EP_E4M3 cache serves both types, others their
+ * own.
+ *   work  device, at least ep_cache_attention_bytes(a, c, p) bytes, 16-byte
+ *         aligned (NULL if that is 0); holds nothing between calls. Calls that
+ *         may overlap need their own.
+ * Errors: EP_EINVAL, EP_EDEVICE.
+ */
+int ep_cache_attention(const ep_attn* a, const ep_cache* c, const ep_pages* p, ep_rows q,
+                       ep_rows out, float* lse, void* work, int64_t work_bytes,
+                       void* hip_stream);
+/* Bytes of work for a call, or EP_EINVAL. */
+int64_t ep_cache_attention_bytes(const ep_attn* a, const ep_cache* c, const ep_pages* p);
 
 /* Wait for all work of the context; reports deferred device errors
  * (EP_EDEVICE) and out-of-range batch indices seen since the last call

@@ -23,6 +23,7 @@ EP_SOLVER_AUTO, EP_SOLVER_DENSE, EP_SOLVER_SUBSPACE = 0, 1, 2
 EP_CONTRACT_AUTO, EP_CONTRACT_FUSED, EP_CONTRACT_BLOCKED = 0, 1, 2
 CONTRACTIONS = {"auto": EP_CONTRACT_AUTO, "fused": EP_CONTRACT_FUSED,
                 "blocked": EP_CONTRACT_BLOCKED}
+EP_BF16, EP_FP16, EP_E4M3 = 0, 1, 2
 EP_PASS_FLOAT32, EP_PASS_SPLIT, EP_PASS_BLOCKED = 0, 1, 2
 SOLVERS = {"auto": EP_SOLVER_AUTO, "dense": EP_SOLVER_DENSE, "subspace": EP_SOLVER_SUBSPACE}
 KERNELS = {"gaussian": EP_GAUSSIAN, "laplacian": EP_LAPLACIAN}
@@ -58,6 +59,30 @@ class EpTiming(ctypes.Structure):
                 ("gemm_ms", ctypes.c_double), ("gemm_launches", ctypes.c_int64)]
 
 
+class EpRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class EpAttn(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("causal", ctypes.c_int32), ("batch", ctypes.c_int64),
+                ("heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("tokens_q", ctypes.c_int64), ("tokens_k", ctypes.c_int64),
+                ("window", ctypes.c_int64), ("start_q", ctypes.c_void_p),
+                ("start_k", ctypes.c_void_p), ("scale", ctypes.c_float)]
+
+
+class EpCacheDesc(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int64),
+                ("kv_heads", ctypes.c_int64), ("dim", ctypes.c_int64), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)]
+
+
+class EpPages(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("table", ctypes.c_void_p), ("cols", ctypes.c_int64),
+                ("lengths", ctypes.c_void_p), ("err", ctypes.c_void_p)]
+
+
 class EigenProError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{_CODES.get(code, code)}: {msg}")
@@ -74,6 +99,7 @@ def _load():
     import torch  # noqa: F401
     lib = ctypes.CDLL(LIB_PATH)
     P, I64, I, F = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
+    PA, PC, PP = (ctypes.POINTER(t) for t in (EpAttn, EpCacheDesc, EpPages))
     sig = {
         "ep_setup": (I, [ctypes.POINTER(P), P, I64, I64, I64, I, F, I64, I64, P,
                          ctypes.c_uint64, P, ctypes.POINTER(EpInfo)]),
@@ -101,6 +127,14 @@ def _load():
                               ctypes.POINTER(ctypes.c_double)]),
         "ep_timing_enable": (I, [P, I]),
         "ep_timing_read": (I, [P, ctypes.POINTER(EpTiming)]),
+        "ep_attention": (I, [PA, EpRows, EpRows, EpRows, EpRows, P, P]),
+        "ep_attention_backward_bytes": (I64, [PA]),
+        "ep_attention_backward": (I, [PA, EpRows, EpRows, EpRows, EpRows, EpRows, P, EpRows,
+                                      EpRows, EpRows, P, I64, P]),
+        "ep_cache_write": (I, [PC, PP, I, EpRows, EpRows, I64, P, P]),
+        "ep_cache_read": (I, [PC, PP, I, EpRows, EpRows, I64, P, P]),
+        "ep_cache_attention_bytes": (I64, [PA, PC, PP]),
+        "ep_cache_attention": (I, [PA, PC, PP, EpRows, EpRows, P, P, I64, P]),
         "ep_sync": (I, [P]),
         "ep_device_probe": (I, [P, P]),
         "ep_destroy": (None, [P]),
@@ -344,6 +378,197 @@ def ep_device_probe():
     mhz = ctypes.c_double()
     _check(_lib.ep_device_probe(ctypes.byref(tf), ctypes.byref(mhz)))
     return tf.value, mhz.value
+
+
+# ---- attention over packed sequences and over a paged cache ----
+
+
+def _rows(x, name, shape, like):
+    """EpRows of a [tokens, heads, dim] tensor; its last axis is contiguous,
+    the others may be strided (slices of a wider array)."""
+    if not x.is_cuda or x.device != like.device:
+        raise ValueError(f"{name}: expected a tensor on {like.device}")
+    if x.dtype != like.dtype:
+        raise TypeError(f"{name}: expected {like.dtype}, got {x.dtype}")
+    if tuple(x.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+    row, head, one = x.stride()
+    if one != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    return EpRows(x.data_ptr(), row, head)
+
+
+def _dense(x, name, dtype, shape, device):
+    """Address of a contiguous tensor of that type, shape and device."""
+    if not x.is_cuda or x.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}")
+    if x.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {x.dtype}")
+    if tuple(x.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+    return x.data_ptr()
+
+
+def _attn_type(x):
+    torch = _torch()
+    if x.dtype == torch.bfloat16:
+        return EP_BF16
+    if x.dtype == torch.float16:
+        return EP_FP16
+    raise TypeError(f"expected bfloat16 or float16, got {x.dtype}")
+
+
+def _attn(q, kv_heads, tokens_k, start_q, start_k, scale, causal, window):
+    torch = _torch()
+    if q.dim() != 3:
+        raise ValueError("q: expected [tokens, heads, dim]")
+    tokens_q, heads, dim = q.shape
+    batch = start_q.shape[0] - 1
+    return EpAttn(_attn_type(q), 1 if causal else 0, batch, heads, kv_heads, dim, tokens_q,
+                  tokens_k, window,
+                  _dense(start_q, "start_q", torch.int32, (batch + 1,), q.device),
+                  None if start_k is None else
+                  _dense(start_k, "start_k", torch.int32, (batch + 1,), q.device),
+                  dim ** -0.5 if scale is None else scale)
+
+
+def _on_stream(device, stream, call):
+    """call(stream handle, allocate) with the tensors' device current; memory
+    from allocate(bytes) belongs to the stream that the work goes to."""
+    torch = _torch()
+    if stream is None and device.index == torch.cuda.current_device():
+        return call(torch.cuda.current_stream().cuda_stream,
+                    lambda n: torch.empty(n, dtype=torch.uint8, device=device))
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.device(device), torch.cuda.stream(stream):
+        return call(torch.cuda.current_stream().cuda_stream,
+                    lambda n: torch.empty(n, dtype=torch.uint8, device=device))
+
+
+def _bytes(n):
+    if n < 0:
+        _check(int(n))
+    return n
+
+
+def ep_attention(q, k, v, out, lse, start_q, start_k, scale=None, causal=True, window=0,
+                 stream=None):
+    """out = softmax(scale q k^T) v over packed sequences, lse its log-sums
+    (float32 [tokens, heads], or None). q, out: [tokens, heads, dim] bfloat16
+    or float16; k, v: [tokens_k, kv_heads, dim]; start_q, start_k: int32,
+    batch + 1 values. scale: dim ** -0.5 by default; window: 0 for none."""
+    torch = _torch()
+    a = _attn(q, k.shape[1], k.shape[0], start_q, start_k, scale, causal, window)
+    kv = (a.tokens_k, a.kv_heads, a.dim)
+    args = (_rows(q, "q", tuple(q.shape), q), _rows(k, "k", kv, q), _rows(v, "v", kv, q),
+            _rows(out, "out", tuple(q.shape), q),
+            None if lse is None else
+            _dense(lse, "lse", torch.float32, tuple(q.shape[:2]), q.device))
+    return _on_stream(q.device, stream, lambda s, _: _check(
+        _lib.ep_attention(ctypes.byref(a), *args, s)))
+
+
+def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k, scale=None,
+                          causal=True, window=0, stream=None):
+    """Gradients dq, dk, dv of ep_attention for the gradient dout of out; out
+    and lse are what it returned. Written, not added to."""
+    torch = _torch()
+    a = _attn(q, k.shape[1], k.shape[0], start_q, start_k, scale, causal, window)
+    qs, kv = tuple(q.shape), (a.tokens_k, a.kv_heads, a.dim)
+    ins = (_rows(dout, "dout", qs, q), _rows(q, "q", qs, q), _rows(k, "k", kv, q),
+           _rows(v, "v", kv, q), _rows(out, "out", qs, q),
+           _dense(lse, "lse", torch.float32, qs[:2], q.device))
+    outs = (_rows(dq, "dq", qs, q), _rows(dk, "dk", kv, q), _rows(dv, "dv", kv, q))
+
+    def call(s, allocate):
+        n = _bytes(_lib.ep_attention_backward_bytes(ctypes.byref(a)))
+        work = allocate(n)
+        return _check(_lib.ep_attention_backward(ctypes.byref(a), *ins, *outs, work.data_ptr(), n,
+                                                 s))
+    return _on_stream(q.device, stream, call)
+
+
+class EpCache:
+    """A paged cache: k_pages and v_pages are [pages, page_size, kv_heads, dim]
+    bfloat16, float16, or float8_e4m3fn (uint8 is taken as that) with float32
+    k_scale and v_scale [pages, page_size, kv_heads]. Holds the tensors."""
+
+    def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
+        torch = _torch()
+        if k_pages.dim() != 4:
+            raise ValueError("k_pages: expected [pages, page_size, kv_heads, dim]")
+        self.tensors = (k_pages, v_pages, k_scale, v_scale)
+        self.device = k_pages.device
+        eight = k_pages.dtype in (torch.float8_e4m3fn, torch.uint8)
+        shape = tuple(k_pages.shape)
+        scales = (None, None)
+        if eight:
+            if k_scale is None or v_scale is None:
+                raise ValueError("an 8-bit cache needs k_scale and v_scale")
+            scales = tuple(_dense(x, n, torch.float32, shape[:3], self.device)
+                           for x, n in ((k_scale, "k_scale"), (v_scale, "v_scale")))
+        pages = tuple(_dense(x, n, k_pages.dtype, shape, self.device)
+                      for x, n in ((k_pages, "k_pages"), (v_pages, "v_pages")))
+        self.desc = EpCacheDesc(EP_E4M3 if eight else _attn_type(k_pages), *shape, *pages, *scales)
+
+
+def _pages(cache, table, lengths, err):
+    torch = _torch()
+    if table.dim() != 2:
+        raise ValueError("table: expected [batch, cols]")
+    batch, cols = table.shape
+    return EpPages(batch, _dense(table, "table", torch.int32, (batch, cols), cache.device), cols,
+                   _dense(lengths, "lengths", torch.int32, (batch,), cache.device),
+                   None if err is None else
+                   _dense(err, "err", torch.int32, (1,), cache.device))
+
+
+def _cache_move(fn, cache, k, v, table, lengths, start, err, stream):
+    torch = _torch()
+    if k.device != cache.device:
+        raise ValueError(f"k: expected a tensor on {cache.device}")
+    p = _pages(cache, table, lengths, err)
+    shape = (k.shape[0], cache.desc.kv_heads, cache.desc.dim)
+    args = (_attn_type(k), _rows(k, "k", shape, k), _rows(v, "v", shape, k), shape[0],
+            _dense(start, "start", torch.int32, (p.batch + 1,), cache.device))
+    return _on_stream(cache.device, stream, lambda s, _: _check(
+        fn(ctypes.byref(cache.desc), ctypes.byref(p), *args, s)))
+
+
+def ep_cache_write(cache, k, v, table, lengths, start, err=None, stream=None):
+    """New tokens k, v [tokens, kv_heads, dim] into their pages; lengths
+    [batch] count them already. err: int32 [1], set to 1 on a bad page."""
+    return _cache_move(_lib.ep_cache_write, cache, k, v, table, lengths, start, err, stream)
+
+
+def ep_cache_read(cache, k, v, table, lengths, start, err=None, stream=None):
+    """Cached tokens back into packed rows k, v: row start[b] + j gets token j
+    of sequence b."""
+    return _cache_move(_lib.ep_cache_read, cache, k, v, table, lengths, start, err, stream)
+
+
+def ep_cache_attention(q, cache, out, lse, table, lengths, start_q, scale=None, causal=True,
+                       window=0, err=None, stream=None):
+    """ep_attention of new tokens' queries over the cached keys and values
+    (theirs included: write them first)."""
+    torch = _torch()
+    if q.device != cache.device:
+        raise ValueError(f"q: expected a tensor on {cache.device}")
+    a = _attn(q, cache.desc.kv_heads, 0, start_q, None, scale, causal, window)
+    p = _pages(cache, table, lengths, err)
+    args = (_rows(q, "q", tuple(q.shape), q), _rows(out, "out", tuple(q.shape), q),
+            None if lse is None else
+            _dense(lse, "lse", torch.float32, tuple(q.shape[:2]), q.device))
+    refs = (ctypes.byref(a), ctypes.byref(cache.desc), ctypes.byref(p))
+
+    def call(s, allocate):
+        n = _bytes(_lib.ep_cache_attention_bytes(*refs))
+        work = allocate(n) if n else None
+        return _check(_lib.ep_cache_attention(*refs, *args, work.data_ptr() if n else None, n, s))
+    return _on_stream(q.device, stream, call)
 
 
 def ep_sync(ctx):

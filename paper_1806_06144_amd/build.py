@@ -16,7 +16,7 @@ SRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libeigenpro.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["api.hip", "kmv.hip", "skmv.hip", "kblock.hip", "kernels.hip", "thin_gemm.hip", "probe.hip",
-           "eigsolve.hip"]
+           "eigsolve.hip", "attention.hip", "attention_backward.hip", "cache.hip", "attn_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

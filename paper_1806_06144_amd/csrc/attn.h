@@ -1,0 +1,280 @@
+// Attention over packed sequences and over a paged cache: arguments of the
+// kernels, and the device code they share.
+//
+// Rows. The heads of a group share their keys, so a work item is a range of
+// the rows (token, head of the group) of one sequence and one key head: row
+// r is token r / group, head r % group. A tile of rows then spans few tokens,
+// which keeps causal tiles narrow, reads every key once per group, and fills
+// a matrix instruction from a single token of many heads.
+//
+// Tiles of 16-bit rows lie in LDS row by row, quads (16 bytes) permuted by
+// quad ^ swizzle(row) since neither the padded rows nor another order can be
+// had from loads that write LDS directly. Two kinds of reads have to be
+// spread over the banks: 16-byte reads of one quad of consecutive rows (eight
+// lanes a cycle, so the swizzle takes eight values over eight rows), and the
+// transposing reads, where 16 lanes read four rows x 32 contiguous bytes (so
+// bits 1 and 2 of the swizzle take four values over four rows).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_index.h"
+#include "ep_device.h"
+#include "split.h"
+
+namespace ep {
+
+struct Rows {                 // element (t, h, c) at p[t row + h head + c]
+    char* p;                  // 16-bit elements; strides in bytes
+    int64_t row, head;
+};
+
+struct AttnArgs {
+    Rows q, k, v, o;          // o: out; the gradients' kernels use the rest
+    Rows dout, dq, dk, dv;
+    float* lse;               // [tokens_q][heads], may be NULL where written
+    float* delta;             // [tokens_q][heads]: sum of out * dout per row
+    const int* start_q;       // batch + 1
+    const int* start_k;       // batch + 1 (packed keys)
+    int64_t tokens_q, tokens_k;
+    int batch, heads, kv_heads, group;
+    unsigned group_magic;     // (attn_index.h)
+    int dim;
+    float scale, scale_log2;  // scale, scale * log2(e)
+    int causal;
+    int window;               // 0: none
+    // paged keys (k.p, v.p: the pages; e4m3 pages: one byte an element)
+    const int* table;
+    int64_t cols;
+    const int* lengths;
+    int pages, page_shift;
+    const float* k_scale;
+    const float* v_scale;
+    int* err;                 // may be NULL
+};
+
+// Workgroups of a launch over tiles of `size` rows.
+inline int64_t attn_groups(int64_t kv_heads, int64_t rows, int64_t size, int64_t batch) {
+    return kv_heads * (rows / size + batch);
+}
+constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // of 256 threads: below 2^32
+
+enum { kPacked = 0, kPaged = 1, kPaged8 = 2 };
+
+hipError_t attn_forward_launch(const AttnArgs& a, bool bf, int source, hipStream_t s);
+hipError_t attn_backward_launch(const AttnArgs& a, bool bf, hipStream_t s);
+
+struct CacheArgs {
+    Rows k, v;                // rows written from or read into
+    char* kp;                 // pages: [page][slot][head][dim]
+    char* vp;
+    float* ks;                // scales [page][slot][head] (e4m3)
+    float* vs;
+    const int* table;
+    int64_t cols;
+    const int* lengths;
+    const int* start;
+    int64_t tokens;
+    int batch, kv_heads, dim, pages, page_shift;
+    int* err;
+};
+hipError_t cache_write_launch(const CacheArgs& a, bool bf, bool e4m3, hipStream_t s);
+hipError_t cache_read_launch(const CacheArgs& a, bool bf, bool e4m3, hipStream_t s);
+
+// ---- device code ----
+
+// Workgroups are numbered key head first: those of one head are 8 apart where
+// kv_heads is a multiple of 8, and so run on one XCD (workgroups go to the 8
+// XCDs round robin), whose L2 then holds few heads' keys. tiles: of the launch.
+__device__ __forceinline__ void head_and_tile(int kv_heads, int& head, int& tile, int& tiles) {
+    head = blockIdx.x % kv_heads;
+    tile = blockIdx.x / kv_heads;
+    tiles = gridDim.x / kv_heads;
+}
+
+constexpr int kRowTile = 128;         // rows of a workgroup: 32 per wave
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+
+template <bool BF>
+__device__ __forceinline__ floatx16 mfma16(uintx4 a, uintx4 b, floatx16 c) {
+    if constexpr (BF)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                       __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a),
+                                                      __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+
+// Two floats rounded to nearest, the first in the low half.
+template <bool BF>
+__device__ __forceinline__ unsigned pack16(float a, float b) {
+    if constexpr (BF) return pack_bf16(a, b);
+    const floatx2 v = {a, b};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(v, half2v));
+}
+template <bool BF>
+__device__ __forceinline__ float lo16(unsigned u) {
+    if constexpr (BF) return bf16_lo(u);
+    return (float)__builtin_bit_cast(half2v, u)[0];
+}
+template <bool BF>
+__device__ __forceinline__ float hi16(unsigned u) {
+    if constexpr (BF) return bf16_hi(u);
+    return (float)__builtin_bit_cast(half2v, u)[1];
+}
+
+// The values of the two lanes (l % 32, l % 32 + 32) that share a row. (The
+// elements are copied before the cast: __builtin_bit_cast of a vector's
+// element takes the first one.)
+__device__ __forceinline__ void pair_of(float x, float& a, float& b) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned lo = r[0], hi = r[1];
+    a = __builtin_bit_cast(float, lo);
+    b = __builtin_bit_cast(float, hi);
+}
+__device__ __forceinline__ float pair_sum(float x) {
+    float a, b;
+    pair_of(x, a, b);
+    return a + b;
+}
+__device__ __forceinline__ float pair_max(float x) {
+    float a, b;
+    pair_of(x, a, b);
+    return fmaxf(a, b);
+}
+
+template <int QUADS>                  // quads a row (16 or 8)
+__device__ __forceinline__ int swizzle(int row) {
+    const int f = ((row & 3) << 1) | ((row >> 2) & 1);
+    return QUADS == 16 ? f | (row & 8) : f;
+}
+template <int QUADS>
+__device__ __forceinline__ int tile_quad(int row, int quad) {
+    return row * QUADS + (quad ^ swizzle<QUADS>(row));
+}
+
+// Operand of 32 rows x 16 depth, the rows those of the tile from row0 on:
+// lane l holds row l % 32, depth 16 step + 8 (l / 32) .. + 7.
+template <int QUADS>
+__device__ __forceinline__ uintx4 tile_rows(const uintx4* tile, int row0, int step, int lane) {
+    return tile[tile_quad<QUADS>(row0 + (lane & 31), 2 * step + (lane >> 5))];
+}
+
+// Operand of 32 columns (from column 32 block on) x 16 rows (from row0 on)
+// of the tile, transposed: lane l holds column l % 32 and rows 4 h .. 4 h + 3,
+// 8 + 4 h .. 8 + 4 h + 3 (h = l / 32) of the sixteen: the order in which a
+// lane's accumulators 8 i .. 8 i + 7 hold the rows of a 32 x 32 product.
+// A transposing read gives lane i of 16 column i of the four rows that lanes
+// 0..3, 4..7, 8..11, 12..15 address.
+template <int QUADS>
+__device__ __forceinline__ uintx4 tile_columns(const uintx4* tile, int row0, int block, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    const int r = 4 * (g >> 1) + (i >> 2);                       // row0 is a multiple of 16
+    const int quad = 4 * block + 2 * (g & 1) + ((i & 3) >> 1);
+    const char* t = reinterpret_cast<const char*>(tile);
+    const char* a = t + ((row0 + r) * QUADS + (quad ^ swizzle<QUADS>(r))) * 16 + (i & 1) * 8;
+    const char* b = t + ((row0 + r + 8) * QUADS + (quad ^ swizzle<QUADS>(r + 8))) * 16 + (i & 1) * 8;
+    const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)a);
+    const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)b);
+    typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+    const uintx2 u = __builtin_bit_cast(uintx2, x), w = __builtin_bit_cast(uintx2, y);
+    return uintx4{u[0], u[1], w[0], w[1]};
+}
+
+// One sequence as a workgroup sees it. Starts and lengths come from device
+// memory: they are held within their arrays whatever they are.
+struct Seq {
+    int b;
+    int q0, n;                // first packed query row (token) and their number
+    int k0, m;                // first packed key row (packed keys) and their number
+    int tile;                 // tile of rows
+    int rows;                 // n * group
+    int off;                  // position of query 0: m - n
+};
+
+// The sequence of tile `t` of the launch, and its first tile.
+__device__ __forceinline__ int find_seq(const int* start, int64_t tokens, int batch, int per,
+                                        int size, int t, int& first) {
+    const int lane = threadIdx.x & 63;
+    int count = 0;
+    for (int i = 0; i < batch; i += 64) {
+        const int b = i + lane;
+        int begin = INT32_MAX;
+        if (b < batch) begin = (int)first_tile(start[b], (int)tokens, b, per, size);
+        count += __builtin_popcountll(__ballot(begin <= t));
+    }
+    const int b = __builtin_amdgcn_readfirstlane(max(count - 1, 0));
+    first = (int)first_tile(start[b], (int)tokens, b, per, size);
+    return b;
+}
+
+template <int SOURCE>
+__device__ __forceinline__ void seq_bounds(const AttnArgs& a, int b, Seq& s) {
+    s.b = b;
+    held_range(a.start_q[b], a.start_q[b + 1], (int)a.tokens_q, s.q0, s.n);
+    if constexpr (SOURCE == kPacked) {
+        held_range(a.start_k[b], a.start_k[b + 1], (int)a.tokens_k, s.k0, s.m);
+    } else {
+        const int length = a.lengths[b];
+        s.k0 = 0;
+        s.m = held_length(length, a.cols, a.page_shift);
+        if (s.m != length && a.err) *a.err = 1;
+    }
+    s.rows = s.n * a.group;
+    s.off = s.m - s.n;
+}
+
+__device__ __forceinline__ int row_token(const AttnArgs& a, int r) {
+    return row_token(r, a.group, a.group_magic);
+}
+__device__ __forceinline__ int key_hi(const AttnArgs& a, const Seq& s, int t) {
+    return visible_hi(t, s.off, s.m, a.causal);
+}
+__device__ __forceinline__ int key_lo(const AttnArgs& a, const Seq& s, int t) {
+    return visible_lo(t, s.off, a.window);
+}
+
+// Where key j of a paged sequence lies: its row in the pages, counted in
+// tokens. Page numbers outside the cache are taken as page 0 and reported.
+__device__ __forceinline__ int64_t page_row(const int* table, int64_t cols, int b, int pages,
+                                            int shift, int* err, int j) {
+    int page = page_of(table, cols, b, pages, shift, j);
+    if (page < 0) {
+        if (err) *err = 1;
+        page = 0;
+    }
+    return page_slot(page, shift, j);
+}
+
+typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+
+// Eight e4m3 values times a power of two as eight 16-bit values (exact).
+template <bool BF>
+__device__ __forceinline__ uintx4 widen8(uintx2 u, float scale) {
+    uintx4 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (BF) {
+            r[2 * i] = __builtin_bit_cast(
+                unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, false));
+            r[2 * i + 1] = __builtin_bit_cast(
+                unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, true));
+        } else {
+            r[2 * i] = __builtin_bit_cast(
+                unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u[i], scale, false));
+            r[2 * i + 1] = __builtin_bit_cast(
+                unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u[i], scale, true));
+        }
+    }
+    return r;
+}
+
+}  // namespace ep

@@ -420,10 +420,16 @@ typedef struct ep_attn {
  *   q    tokens_q x heads x dim.   k, v  tokens_k x kv_heads x dim.
  *   out  as q; must not overlap the inputs.
  *   lse  device float32 tokens_q x heads, or NULL.
- * Errors: EP_EINVAL (the bounds of ep_attn and ep_rows, NULL), EP_EDEVICE.
+ *   work device, at least ep_attention_bytes(a) bytes, 16-byte aligned (NULL if
+ *        that is 0): partial results where few rows meet many keys. It holds
+ *        nothing between calls; calls that may overlap need their own.
+ * Errors: EP_EINVAL (the bounds of ep_attn and ep_rows, NULL, work too small),
+ * EP_EDEVICE.
  */
 int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, ep_rows out, float* lse,
-                 void* hip_stream);
+                 void* work, int64_t work_bytes, void* hip_stream);
+/* Bytes of work for a call, or EP_EINVAL. */
+int64_t ep_attention_bytes(const ep_attn* a);
 
 /*
  * ep_attention_backward — dq, dk, dv for a gradient dout of out. The

@@ -127,7 +127,8 @@ def _load():
                               ctypes.POINTER(ctypes.c_double)]),
         "ep_timing_enable": (I, [P, I]),
         "ep_timing_read": (I, [P, ctypes.POINTER(EpTiming)]),
-        "ep_attention": (I, [PA, EpRows, EpRows, EpRows, EpRows, P, P]),
+        "ep_attention_bytes": (I64, [PA]),
+        "ep_attention": (I, [PA, EpRows, EpRows, EpRows, EpRows, P, P, I64, P]),
         "ep_attention_backward_bytes": (I64, [PA]),
         "ep_attention_backward": (I, [PA, EpRows, EpRows, EpRows, EpRows, EpRows, P, EpRows,
                                       EpRows, EpRows, P, I64, P]),
@@ -467,8 +468,13 @@ def ep_attention(q, k, v, out, lse, start_q, start_k, scale=None, causal=True, w
             _rows(out, "out", tuple(q.shape), q),
             None if lse is None else
             _dense(lse, "lse", torch.float32, tuple(q.shape[:2]), q.device))
-    return _on_stream(q.device, stream, lambda s, _: _check(
-        _lib.ep_attention(ctypes.byref(a), *args, s)))
+
+    def call(s, allocate):
+        n = _bytes(_lib.ep_attention_bytes(ctypes.byref(a)))
+        work = allocate(n) if n else None
+        return _check(_lib.ep_attention(ctypes.byref(a), *args, work.data_ptr() if n else None, n,
+                                        s))
+    return _on_stream(q.device, stream, call)
 
 
 def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k, scale=None,

@@ -15,12 +15,26 @@
 // much as the output's own rounding); their sum is taken before that.
 #include "attn.h"
 #include "ep_internal.h"
+#include "launch.h"
+
+#include <type_traits>
 
 namespace ep {
 
 namespace {
 
 constexpr int kKeys = 64;             // keys of a tile
+constexpr int kWaveKeys = 32;         // keys of a wave's own tile (few rows)
+
+// This workgroup's range of keys: begin .. end, whole tiles of `size`, cut
+// into a.splits ranges.
+__device__ __forceinline__ void split_range(int split, int splits, int size, int& begin, int& end) {
+    const int tiles = (end - begin + size - 1) / size;
+    const int per = (tiles + splits - 1) / splits;
+    const int from = begin + min(split * per, tiles) * size;
+    end = min(end, begin + min((split + 1) * per, tiles) * size);
+    begin = from;
+}
 
 template <bool BF, int DP, int SOURCE>
 __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
@@ -36,7 +50,8 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     const int half = lane >> 5;
     int kvh, tile, tiles, first;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
-    tile = tiles - 1 - tile;                         // long causal tiles first
+    const int split = tile % a.splits;
+    tile = (tiles - 1 - tile) / a.splits;            // long causal tiles first
     Seq s;
     seq_bounds<SOURCE>(a, find_seq(a.start_q, a.tokens_q, a.batch, a.group, kRowTile, tile, first), s);
     const int r0 = (tile - first) * kRowTile;
@@ -64,8 +79,9 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     const int t0 = row_token(a, w0), t1 = row_token(a, w1);
     const int w_lo = key_lo(a, s, t0), w_hi = key_hi(a, s, t1);          // any row sees
     const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);      // every row sees
-    const int begin = key_lo(a, s, row_token(a, r0)) / kKeys * kKeys;
-    const int end = key_hi(a, s, row_token(a, r1));
+    int begin = key_lo(a, s, row_token(a, r0)) / kKeys * kKeys;
+    int end = key_hi(a, s, row_token(a, r1));
+    split_range(split, a.splits, kKeys, begin, end);
 
     floatx16 acc[kBlocks];
 #pragma unroll
@@ -152,6 +168,24 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     if (r0 + wave * 32 + (lane & 31) >= s.rows) return;
     sum = pair_sum(sum);
     const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    const float lse2 = sum == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(sum);
+    if (a.splits > 1) {
+        const int64_t to = ((split * a.tokens_q + at) * a.heads + head);
+        if (half == 0) a.part_lse[to] = lse2;
+        if (sum == 0.f) return;                      // (never read)
+        float* part = a.part + to * a.dim;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * b + 2 * i + 4 * half;
+                if (d < a.dim)
+                    *reinterpret_cast<float4*>(part + d) =
+                        make_float4(acc[b][i] * inv, acc[b][i + 1] * inv, acc[b][i + 2] * inv,
+                                    acc[b][i + 3] * inv);
+            }
+        return;
+    }
     char* op = a.o.p + at * a.o.row + head * a.o.head;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -163,28 +197,289 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
                     uintx2{pack16<BF>(acc[b][i] * inv, acc[b][i + 1] * inv),
                            pack16<BF>(acc[b][i + 2] * inv, acc[b][i + 3] * inv)};
         }
-    if (a.lse && half == 0)
-        a.lse[at * a.heads + head] =
-            sum == 0.f ? -__builtin_inff() : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (a.lse && half == 0) a.lse[at * a.heads + head] = lse2 * kLn2;
+}
+
+// The same pass for few rows: a workgroup's four waves share 32 rows and take
+// the tiles of 32 keys in turn, each with a running maximum and sum of its
+// own, joined at the end. What bounds it is the cache's stream from memory:
+// a wave loads its next tile (up to 16 KB) into registers while it works on
+// the one in its own part of LDS, so there is no barrier before the end, and
+// two workgroups a CU keep up to 128 KB on the way.
+template <bool BF, int DP, int SOURCE>
+__global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
+    constexpr int kQuads = DP / 8;
+    constexpr int kSteps = DP / 16;
+    constexpr int kBlocks = DP / 32;
+    constexpr int kLoads = kWaveKeys * kQuads / 64;  // of K, and of V
+    __shared__ uintx4 tiles_lds[4][2][kWaveKeys * kQuads];
+    __shared__ float s_top[4][32], s_sum[4][32];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5;
+    int kvh, tile, tiles, first;
+    head_and_tile(a.kv_heads, kvh, tile, tiles);
+    const int split = tile % a.splits;
+    tile /= a.splits;
+    Seq s;
+    seq_bounds<SOURCE>(a, find_seq(a.start_q, a.tokens_q, a.batch, a.group, kFewRows, tile, first), s);
+    const int r0 = (tile - first) * kFewRows;
+    if (r0 < 0 || r0 >= s.rows) return;
+    const int r1 = min(r0 + kFewRows, s.rows) - 1;
+
+    const int row = min(r0 + (lane & 31), s.rows - 1);
+    const int tok = row_token(a, row);
+    const int64_t at = s.q0 + tok;
+    const int head = kvh * a.group + (row - tok * a.group);
+    const int hi = key_hi(a, s, tok), lo = key_lo(a, s, tok);
+    uintx4 qf[kSteps];
+    {
+        const char* qp = a.q.p + at * a.q.row + head * a.q.head;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int d = 16 * i + 8 * half;
+            qf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(qp + 2 * d) : uintx4{0, 0, 0, 0};
+        }
+    }
+    const int t0 = row_token(a, r0), t1 = row_token(a, r1);
+    const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);
+    int begin = key_lo(a, s, t0) / kWaveKeys * kWaveKeys;
+    int end = key_hi(a, s, t1);
+    split_range(split, a.splits, 4 * kWaveKeys, begin, end);
+
+    floatx16 acc[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
+    float top = -3.0e38f, sum = 0.f;
+
+    uintx4* kt = tiles_lds[wave][0];
+    uintx4* vt = tiles_lds[wave][1];
+    const int last_quad = a.dim / 8 - 1;
+    typedef std::conditional_t<SOURCE == kPaged8, uintx2, uintx4> Quad;
+    Quad kr[kLoads], vr[kLoads];
+    float ks[kLoads], vs[kLoads];
+    auto load = [&](int j0) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int at_quad = lane + 64 * i;
+            const int r = at_quad / kQuads;
+            const int quad = min((at_quad % kQuads) ^ swizzle<kQuads>(r), last_quad);
+            const int j = min(j0 + r, s.m - 1);
+            const int64_t row = SOURCE == kPacked
+                                    ? (int64_t)(s.k0 + j)
+                                    : page_row(a.table, a.cols, s.b, a.pages, a.page_shift, a.err, j);
+            const int size = sizeof(Quad);
+            kr[i] = *reinterpret_cast<const Quad*>(a.k.p + row * a.k.row + kvh * a.k.head + quad * size);
+            vr[i] = *reinterpret_cast<const Quad*>(a.v.p + row * a.v.row + kvh * a.v.head + quad * size);
+            if constexpr (SOURCE == kPaged8) {
+                ks[i] = a.k_scale[row * a.kv_heads + kvh];
+                vs[i] = a.v_scale[row * a.kv_heads + kvh];
+            }
+        }
+    };
+    int j0 = begin + wave * kWaveKeys;
+    if (j0 < end) load(j0);
+    for (; j0 < end; j0 += 4 * kWaveKeys) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if constexpr (SOURCE == kPaged8) {
+                kt[lane + 64 * i] = widen8<BF>(kr[i], ks[i]);
+                vt[lane + 64 * i] = widen8<BF>(vr[i], vs[i]);
+            } else {
+                kt[lane + 64 * i] = kr[i];
+                vt[lane + 64 * i] = vr[i];
+            }
+        }
+        if (j0 + 4 * kWaveKeys < end) load(j0 + 4 * kWaveKeys);
+        floatx16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+            sc = mfma16<BF>(tile_rows<kQuads>(kt, 0, i, lane), qf[i], sc);
+        if (j0 < all_lo || j0 + kWaveKeys > all_hi) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int j = j0 + 8 * (i >> 2) + 4 * half + (i & 3);
+                if (j < lo || j >= hi) sc[i] = -__builtin_inff();
+            }
+        }
+        float mx = sc[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
+        mx = pair_max(mx) * a.scale_log2;
+        const float now = fmaxf(top, mx);
+        const float shrink = __builtin_amdgcn_exp2f(top - now);
+        top = now;
+        sum *= shrink;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[b][i] *= shrink;
+        uintx4 pf[2];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -top));
+            const float y = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -top));
+            sum += x + y;
+            pf[i >> 3][(i & 7) >> 1] = pack16<BF>(x, y);
+        }
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                acc[b] = mfma16<BF>(tile_columns<kQuads>(vt, 16 * i, b, lane), pf[i], acc[b]);
+    }
+    // Joining: every wave leaves its sums in its part of LDS, row by row of
+    // queries (quads permuted by the row, which spreads a write over the
+    // banks), and 8 threads gather a row.
+    sum = pair_sum(sum);
+    if (half == 0) {
+        s_top[wave][lane] = top;
+        s_sum[wave][lane] = sum;
+    }
+    constexpr int kFloatQuads = DP / 4;
+    float4* mine = reinterpret_cast<float4*>(tiles_lds[wave]);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int quad = 8 * b + (i >> 1) + half;
+            mine[(lane & 31) * kFloatQuads + (quad ^ (lane & 7))] =
+                make_float4(acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]);
+        }
+    __syncthreads();
+    const int q = tid >> 3;
+    if (r0 + q >= s.rows) return;
+    float weight[4], all = -3.0e38f, total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) all = fmaxf(all, s_top[w][q]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        weight[w] = __builtin_amdgcn_exp2f(s_top[w][q] - all);
+        total = fmaf(weight[w], s_sum[w][q], total);
+    }
+    const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
+    const float lse2 = total == 0.f ? -__builtin_inff() : all + __builtin_amdgcn_logf(total);
+    const int qtok = row_token(a, r0 + q);
+    const int qhead = kvh * a.group + (r0 + q - qtok * a.group);
+    const int64_t to = (int64_t)(s.q0 + qtok) * a.heads + qhead;
+    const int64_t to_part = split * a.tokens_q * a.heads + to;
+    if ((tid & 7) == 0) {
+        if (a.splits > 1) a.part_lse[to_part] = lse2;
+        else if (a.lse) a.lse[to] = lse2 * kLn2;
+    }
+    if (a.splits > 1 && total == 0.f) return;        // (never read)
+    char* op = a.o.p + (s.q0 + qtok) * a.o.row + qhead * a.o.head;
+#pragma unroll
+    for (int i = 0; i < kFloatQuads / 8; ++i) {
+        const int quad = (tid & 7) + 8 * i;
+        if (quad * 4 >= a.dim) break;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float4 x = reinterpret_cast<const float4*>(tiles_lds[w])[q * kFloatQuads + (quad ^ (q & 7))];
+            o.x = fmaf(weight[w], x.x, o.x);
+            o.y = fmaf(weight[w], x.y, o.y);
+            o.z = fmaf(weight[w], x.z, o.z);
+            o.w = fmaf(weight[w], x.w, o.w);
+        }
+        if (a.splits > 1)
+            *reinterpret_cast<float4*>(a.part + to_part * a.dim + quad * 4) =
+                make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        else
+            *reinterpret_cast<uintx2*>(op + quad * 8) =
+                uintx2{pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv)};
+    }
+}
+
+// out = sum over the cuts of 2^(lse_s - lse) part_s, in the cuts' order; a
+// thread takes four elements of a row.
+template <bool BF>
+__global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
+    const int quads = a.dim / 4;
+    const int64_t rows = a.tokens_q * a.heads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * quads;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / quads, tok = row / a.heads;
+        const int quad = (int)(i % quads), head = (int)(row % a.heads);
+        // rows behind the last sequence have no partial results
+        if (tok < a.start_q[0] || tok >= a.start_q[a.batch]) continue;
+        float all = -3.0e38f, total = 0.f;
+        for (int s = 0; s < a.splits; ++s) all = fmaxf(all, a.part_lse[s * rows + row]);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < a.splits; ++s) {
+            const float l = a.part_lse[s * rows + row];
+            if (l == -__builtin_inff()) continue;
+            const float w = __builtin_amdgcn_exp2f(l - all);
+            const float4 x = *reinterpret_cast<const float4*>(a.part + (s * rows + row) * a.dim + quad * 4);
+            total += w;
+            o.x = fmaf(w, x.x, o.x);
+            o.y = fmaf(w, x.y, o.y);
+            o.z = fmaf(w, x.z, o.z);
+            o.w = fmaf(w, x.w, o.w);
+        }
+        const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
+        *reinterpret_cast<uintx2*>(a.o.p + tok * a.o.row + head * a.o.head + quad * 8) =
+            uintx2{pack16<BF>(o.x * inv, o.y * inv), pack16<BF>(o.z * inv, o.w * inv)};
+        if (quad == 0 && a.lse)
+            a.lse[row] = total == 0.f ? -__builtin_inff() : (all + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+}
+
+template <bool BF, int DP, int SOURCE>
+void launch_dim(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    const dim3 grid((unsigned)(attn_groups(a.kv_heads, a.tokens_q * a.group, p.tile, a.batch) * p.splits));
+    if (p.tile == kFewRows)
+        hipLaunchKernelGGL((attn_few_kernel<BF, DP, SOURCE>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_kernel<BF, DP, SOURCE>), grid, dim3(256), 0, s, a);
 }
 
 template <bool BF, int SOURCE>
-void launch(const AttnArgs& a, dim3 grid, hipStream_t s) {
-    if (a.dim > 64) hipLaunchKernelGGL((attn_kernel<BF, 128, SOURCE>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_kernel<BF, 64, SOURCE>), grid, dim3(256), 0, s, a);
+void launch(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
+    if (a.dim > 64) launch_dim<BF, 128, SOURCE>(a, p, s);
+    else launch_dim<BF, 64, SOURCE>(a, p, s);
 }
 
 }  // namespace
 
-hipError_t attn_forward_launch(const AttnArgs& a, bool bf, int source, hipStream_t s) {
-    const dim3 grid((unsigned)attn_groups(a.kv_heads, a.tokens_q * a.group, kRowTile, a.batch));
+AttnPlan attn_plan(int64_t batch, int64_t tokens_q, int64_t heads, int64_t kv_heads, int64_t dim,
+                   int64_t most_keys) {
+    AttnPlan p;
+    const int64_t rows = tokens_q * (heads / kv_heads);
+    const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_q), 1);
+    p.tile = rows <= kFewRows * sequences ? kFewRows : kRowTile;
+    // Workgroups that have work, if no sequence is much longer than the
+    // others; cut the keys until the device is full: its 512 slots four times
+    // over for few rows (ragged lengths even out), once for many.
+    const int64_t groups = kv_heads * std::max(sequences, ceil_div(rows, p.tile));
+    const int64_t want = p.tile == kFewRows ? 2048 : 512;
+    const int64_t least = p.tile == kFewRows ? 4 * kWaveKeys : 4 * kKeys;
+    p.splits = (int)std::max<int64_t>(
+        1, std::min({want / groups, most_keys / least, int64_t(128),
+                     kMaxGroups / attn_groups(kv_heads, rows, p.tile, batch)}));
+    p.bytes = p.splits > 1 ? round_up(p.splits * tokens_q * heads * (dim + 1) * 4, 16) : 0;
+    return p;
+}
+
+hipError_t attn_forward_launch(const AttnArgs& a, const AttnPlan& p, bool bf, int source,
+                               hipStream_t s) {
     switch (source * 2 + (bf ? 1 : 0)) {
-    case 0: launch<false, kPacked>(a, grid, s); break;
-    case 1: launch<true, kPacked>(a, grid, s); break;
-    case 2: launch<false, kPaged>(a, grid, s); break;
-    case 3: launch<true, kPaged>(a, grid, s); break;
-    case 4: launch<false, kPaged8>(a, grid, s); break;
-    default: launch<true, kPaged8>(a, grid, s); break;
+    case 0: launch<false, kPacked>(a, p, s); break;
+    case 1: launch<true, kPacked>(a, p, s); break;
+    case 2: launch<false, kPaged>(a, p, s); break;
+    case 3: launch<true, kPaged>(a, p, s); break;
+    case 4: launch<false, kPaged8>(a, p, s); break;
+    default: launch<true, kPaged8>(a, p, s); break;
+    }
+    if (p.splits > 1) {
+        const dim3 grid(stride_grid(ceil_div(a.tokens_q * a.heads * (a.dim / 4), 256), 256));
+        if (bf) hipLaunchKernelGGL(attn_join_kernel<true>, grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL(attn_join_kernel<false>, grid, dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }

@@ -52,17 +52,35 @@ struct AttnArgs {
     const float* k_scale;
     const float* v_scale;
     int* err;                 // may be NULL
+    // keys cut into `splits` ranges: normalised partial outputs
+    // [splits][tokens_q][heads][dim] and their log-sums, in units of log 2
+    int splits;
+    float* part;
+    float* part_lse;
 };
+
+// How a forward pass runs: rows of a tile (32: the four waves of a workgroup
+// share the rows and split the keys; 128: 32 rows each), and cuts of the keys.
+struct AttnPlan {
+    int tile;
+    int splits;
+    int64_t bytes;            // of partial results
+};
+AttnPlan attn_plan(int64_t batch, int64_t tokens_q, int64_t heads, int64_t kv_heads, int64_t dim,
+                   int64_t most_keys);
 
 // Workgroups of a launch over tiles of `size` rows.
 inline int64_t attn_groups(int64_t kv_heads, int64_t rows, int64_t size, int64_t batch) {
     return kv_heads * (rows / size + batch);
 }
+constexpr int kRowTile = 128;         // rows of a workgroup: 32 per wave
+constexpr int kFewRows = 32;          // rows of a workgroup whose waves split the keys
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // of 256 threads: below 2^32
 
 enum { kPacked = 0, kPaged = 1, kPaged8 = 2 };
 
-hipError_t attn_forward_launch(const AttnArgs& a, bool bf, int source, hipStream_t s);
+hipError_t attn_forward_launch(const AttnArgs& a, const AttnPlan& p, bool bf, int source,
+                               hipStream_t s);
 hipError_t attn_backward_launch(const AttnArgs& a, bool bf, hipStream_t s);
 
 struct CacheArgs {
@@ -92,8 +110,6 @@ __device__ __forceinline__ void head_and_tile(int kv_heads, int& head, int& tile
     tile = blockIdx.x / kv_heads;
     tiles = gridDim.x / kv_heads;
 }
-
-constexpr int kRowTile = 128;         // rows of a workgroup: 32 per wave
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 

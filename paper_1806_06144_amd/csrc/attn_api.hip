@@ -32,11 +32,11 @@ int check_attn(const ep_attn* a, bool packed_keys) {
     const int64_t group = a->heads / a->kv_heads;
     REQUIRE(a->tokens_q * group * group < int64_t(1) << 32,
             "tokens_q * (heads / kv_heads)^2 must be below 2^32");
-    REQUIRE(attn_groups(a->kv_heads, a->tokens_q * group, kRowTile, a->batch) <= kMaxGroups &&
+    REQUIRE(attn_groups(a->kv_heads, a->tokens_q * group, kFewRows, a->batch) <= kMaxGroups &&
                 (!packed_keys ||
                  attn_groups(a->kv_heads, a->tokens_k, kRowTile, a->batch) <= kMaxGroups),
-            "too many workgroups: kv_heads * (tokens * (heads / kv_heads) / 128 + batch) must be "
-            "below 2^24");
+            "too many workgroups: kv_heads * (tokens_q * (heads / kv_heads) / 32 + batch) and "
+            "kv_heads * (tokens_k / 128 + batch) must be below 2^24");
     REQUIRE(std::isfinite(a->scale) && a->scale > 0.f, "scale must be positive and finite");
     REQUIRE(a->causal == 0 || a->causal == 1, "causal must be 0 or 1");
     REQUIRE(a->window >= 0 && a->window < kMaxTokens, "window must be in [0, 2^30)");
@@ -112,9 +112,31 @@ AttnArgs args_of(const ep_attn* a) {
     return g;
 }
 
-// (size 0: no device work is needed, and a grid must not be empty)
+// Where a plan's partial results go.
+void set_plan(AttnArgs& g, const AttnPlan& p, void* work) {
+    g.splits = p.splits;
+    g.part = static_cast<float*>(work);
+    g.part_lse = g.part + (p.splits > 1 ? p.splits * g.tokens_q * g.heads * g.dim : 0);
+}
+
 int launched(hipError_t e) {
     if (e != hipSuccess) return fail(EP_EDEVICE, "launch: %s", hipGetErrorString(e));
+    return EP_OK;
+}
+
+// keys: of a sequence, as far as the host can tell.
+AttnPlan plan_of(const ep_attn* a, int64_t keys) {
+    if (a->window) keys = std::min(keys, a->window + kRowTile);
+    return attn_plan(a->batch, a->tokens_q, a->heads, a->kv_heads, a->dim, keys);
+}
+// Packed sequences: twice the average, for ragged ones.
+AttnPlan plan_packed(const ep_attn* a) {
+    return plan_of(a, std::min(a->tokens_k, 2 * ceil_div(a->tokens_k, a->batch)));
+}
+
+int check_work(const void* work, int64_t bytes, int64_t need) {
+    REQUIRE(bytes >= need && (work || need == 0) && aligned16(work),
+            "work must be 16-byte aligned and hold %lld bytes", (long long)need);
     return EP_OK;
 }
 
@@ -161,21 +183,29 @@ int check_cached(const ep_attn* a, const ep_cache* c, const ep_pages* p) {
 
 }  // namespace
 
+extern "C" int64_t ep_attention_bytes(const ep_attn* a) {
+    TRY(check_attn(a, true));
+    return plan_packed(a).bytes;
+}
+
 extern "C" int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, ep_rows out,
-                            float* lse, void* hip_stream) {
+                            float* lse, void* work, int64_t work_bytes, void* hip_stream) {
     TRY(check_attn(a, true));
     TRY(check_rows("q", q, a->tokens_q));
     TRY(check_rows("out", out, a->tokens_q));
     TRY(check_rows("k", k, a->tokens_k));
     TRY(check_rows("v", v, a->tokens_k));
+    const AttnPlan plan = plan_packed(a);
+    TRY(check_work(work, work_bytes, plan.bytes));
     if (a->tokens_q == 0) return EP_OK;
     AttnArgs g = args_of(a);
+    set_plan(g, plan, work);
     g.q = rows_of(q);
     g.k = rows_of(k);
     g.v = rows_of(v);
     g.o = rows_of(out);
     g.lse = lse;
-    return launched(attn_forward_launch(g, a->type == EP_BF16, kPacked,
+    return launched(attn_forward_launch(g, plan, a->type == EP_BF16, kPacked,
                                         static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -198,8 +228,7 @@ extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, 
     }
     REQUIRE(lse || a->tokens_q == 0, "lse is NULL");
     const int64_t need = ep_attention_backward_bytes(a);
-    REQUIRE(work_bytes >= need && (work || need == 0) && aligned16(work),
-            "work must be 16-byte aligned and hold %lld bytes", (long long)need);
+    TRY(check_work(work, work_bytes, need));
     AttnArgs g = args_of(a);
     g.dout = rows_of(dout);
     g.q = rows_of(q);
@@ -234,7 +263,7 @@ extern "C" int ep_cache_read(const ep_cache* c, const ep_pages* p, int type, ep_
 extern "C" int64_t ep_cache_attention_bytes(const ep_attn* a, const ep_cache* c,
                                             const ep_pages* p) {
     TRY(check_cached(a, c, p));
-    return 0;
+    return plan_of(a, p->cols * c->page_size).bytes;
 }
 
 extern "C" int ep_cache_attention(const ep_attn* a, const ep_cache* c, const ep_pages* p,
@@ -243,11 +272,11 @@ extern "C" int ep_cache_attention(const ep_attn* a, const ep_cache* c, const ep_
     TRY(check_cached(a, c, p));
     TRY(check_rows("q", q, a->tokens_q));
     TRY(check_rows("out", out, a->tokens_q));
-    const int64_t need = ep_cache_attention_bytes(a, c, p);
-    REQUIRE(work_bytes >= need && (work || need == 0) && aligned16(work),
-            "work must be 16-byte aligned and hold %lld bytes", (long long)need);
+    const AttnPlan plan = plan_of(a, p->cols * c->page_size);
+    TRY(check_work(work, work_bytes, plan.bytes));
     if (a->tokens_q == 0) return EP_OK;
     AttnArgs g = args_of(a);
+    set_plan(g, plan, work);
     const int64_t bytes = c->type == EP_E4M3 ? 1 : 2;
     g.q = rows_of(q);
     g.o = rows_of(out);
@@ -262,6 +291,6 @@ extern "C" int ep_cache_attention(const ep_attn* a, const ep_cache* c, const ep_
     g.pages = (int)c->pages;
     g.page_shift = shift_of(c->page_size);
     g.err = p->err;
-    return launched(attn_forward_launch(g, a->type == EP_BF16, c->type == EP_E4M3 ? kPaged8 : kPaged,
+    return launched(attn_forward_launch(g, plan, a->type == EP_BF16, c->type == EP_E4M3 ? kPaged8 : kPaged,
                                         static_cast<hipStream_t>(hip_stream)));
 }

@@ -171,7 +171,7 @@ def _forward(a, **kw):
     r = {n: _rows() for n in ("q", "k", "v", "out")}
     r.update(kw)
     return ep.raw_call("ep_attention", None if a is None else ctypes.byref(a), r["q"], r["k"],
-                       r["v"], r["out"], A, None)
+                       r["v"], r["out"], A, A, 1 << 30, None)
 
 
 BAD = [dict(type=2), dict(type=-1), dict(causal=2), dict(batch=0), dict(batch=1 << 24),

@@ -23,6 +23,9 @@ namespace ep {
 
 namespace {
 
+#ifndef OCC64
+#define OCC64 2
+#endif
 constexpr int kKeys = 64;             // keys of a tile
 constexpr int kWaveKeys = 32;         // keys of a wave's own tile (few rows)
 
@@ -36,14 +39,100 @@ __device__ __forceinline__ void split_range(int split, int splits, int size, int
     begin = from;
 }
 
+// Tiles on their way into LDS, fetched a tile ahead into one of two buffers,
+// so that the loop's only barrier finds them there. Page numbers are looked up
+// a tile before that: a wait for one would wait for the loads before it too.
 template <bool BF, int DP, int SOURCE>
-__global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
+struct KeyTiles {
+    static constexpr int kQuads = DP / 8;
+    static constexpr int kLoads = TileLoader<kQuads>::kLoads;
+    static constexpr bool kEight = SOURCE == kE4m3 || SOURCE == kE4m3Small;
+    static constexpr bool kSmall = SOURCE == kPagedSmall || SOURCE == kE4m3Small;
+    const AttnArgs& a;
+    const Seq& s;
+    const int wave, lane, kvh;
+    const TileLoader<kQuads> l;
+    int page[kSmall ? kLoads : 1];    // of the wave's rows (of a load's) in the next tile
+    // e4m3: the next tile, held in registers until it can be widened
+    uintx2 k8[kLoads], v8[kLoads];
+    float ks[kLoads], vs[kLoads];
+
+    __device__ __forceinline__ KeyTiles(const AttnArgs& a_, const Seq& s_, int wave_, int lane_, int kvh_)
+        : a(a_), s(s_), wave(wave_), lane(lane_), kvh(kvh_), l(lane_, a_.dim) {}
+
+    __device__ __forceinline__ void look(int j0) {
+        if constexpr (SOURCE == kPacked) return;
+        const int* t = a.table + s.b * a.cols;
+        const int j = j0 + kWaveRows * wave;
+        if constexpr (kSmall) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) page[i] = t[min(j + l.row(i), s.m - 1) >> a.page_shift];
+        } else {
+            page[0] = t[min(j, s.m - 1) >> a.page_shift];
+        }
+    }
+    __device__ __forceinline__ int64_t place(int page, int j) const {
+        if ((unsigned)page >= (unsigned)a.pages) {
+            if (a.err) *a.err = 1;
+            page = 0;
+        }
+        return page_slot(page, a.page_shift, j);
+    }
+    // Starts the loads of tile j0, whose pages were looked up (e4m3: into
+    // registers).
+    __device__ __forceinline__ void fetch(int j0, uintx4* kt, uintx4* vt) {
+        const int j = min(j0 + kWaveRows * wave, s.m - 1);
+        const char* kp = a.k.p + kvh * a.k.head;
+        const char* vp = a.v.p + kvh * a.v.head;
+        uintx4* kto = kt + kWaveRows * kQuads * wave;
+        uintx4* vto = vt + kWaveRows * kQuads * wave;
+        if constexpr (SOURCE == kPacked || SOURCE == kPaged) {
+            int64_t row = s.k0 + j;
+            if constexpr (SOURCE == kPaged) row = place(__builtin_amdgcn_readfirstlane(page[0]), j);
+            l.load(kp + row * a.k.row, s.m - j, a.k.row, kto);
+            l.load(vp + row * a.v.row, s.m - j, a.v.row, vto);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                int64_t row;
+                if constexpr (kSmall) row = place(page[i], min(j + l.row(i), s.m - 1));
+                else row = place(__builtin_amdgcn_readfirstlane(page[0]), j) + min(l.row(i), s.m - 1 - j);
+                if constexpr (kEight) {
+                    k8[i] = *reinterpret_cast<const uintx2*>(kp + row * a.k.row + l.quad(i) / 2);
+                    v8[i] = *reinterpret_cast<const uintx2*>(vp + row * a.v.row + l.quad(i) / 2);
+                    ks[i] = a.k_scale[row * a.kv_heads + kvh];
+                    vs[i] = a.v_scale[row * a.kv_heads + kvh];
+                } else {
+                    load_lds16(kp + row * a.k.row + l.quad(i), kto + 64 * i);
+                    load_lds16(vp + row * a.v.row + l.quad(i), vto + 64 * i);
+                }
+            }
+        }
+    }
+    // Puts what fetch holds in registers into the tile.
+    __device__ __forceinline__ void store(uintx4* kt, uintx4* vt) {
+        if constexpr (kEight) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int to = kWaveRows * kQuads * wave + 64 * i + lane;
+                kt[to] = widen8<BF>(k8[i], ks[i]);
+                vt[to] = widen8<BF>(v8[i], vs[i]);
+            }
+        }
+    }
+};
+
+template <bool BF, int DP, int SOURCE>
+__global__ void __launch_bounds__(256, DP == 64 ? OCC64 : 2) attn_kernel(AttnArgs a) {
     constexpr int kQuads = DP / 8;
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
-    constexpr int kLoads = kKeys * kQuads / 256;
-    __shared__ uintx4 kt[kKeys * kQuads];
-    __shared__ uintx4 vt[kKeys * kQuads];
+    // (arrays of their own: what is loaded into one is not waited for where
+    // another is read)
+    __shared__ uintx4 kt0[kKeys * kQuads];
+    __shared__ uintx4 kt1[kKeys * kQuads];
+    __shared__ uintx4 vt0[kKeys * kQuads];
+    __shared__ uintx4 vt1[kKeys * kQuads];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -64,21 +153,11 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     const int64_t at = s.q0 + tok;
     const int head = kvh * a.group + (row - tok * a.group);
     const int hi = key_hi(a, s, tok), lo = key_lo(a, s, tok);
-    uintx4 qf[kSteps];
-    {
-        const char* qp = a.q.p + at * a.q.row + head * a.q.head;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int d = 16 * i + 8 * half;
-            qf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(qp + 2 * d) : uintx4{0, 0, 0, 0};
-        }
-    }
-    // the wave's and the workgroup's ranges of keys
-    const int w0 = min(r0 + wave * 32, s.rows - 1), w1 = min(r0 + wave * 32 + 31, s.rows - 1);
-    const bool active = r0 + wave * 32 < s.rows;
-    const int t0 = row_token(a, w0), t1 = row_token(a, w1);
-    const int w_lo = key_lo(a, s, t0), w_hi = key_hi(a, s, t1);          // any row sees
-    const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);      // every row sees
+    // keys that every row of the wave sees, and those that any row of the
+    // workgroup does
+    const int t0 = row_token(a, min(r0 + wave * 32, s.rows - 1));
+    const int t1 = row_token(a, min(r0 + wave * 32 + 31, s.rows - 1));
+    const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);
     int begin = key_lo(a, s, row_token(a, r0)) / kKeys * kKeys;
     int end = key_hi(a, s, row_token(a, r1));
     split_range(split, a.splits, kKeys, begin, end);
@@ -90,80 +169,84 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
     float top = -3.0e38f, sum = 0.f;                 // (top: in units of log 2)
 
-    const int last_quad = a.dim / 8 - 1;
-    for (int j0 = begin; j0 < end; j0 += kKeys) {
-        __syncthreads();
+    if (begin < end) {
+        KeyTiles<BF, DP, SOURCE> keys(a, s, wave, lane, kvh);
+        keys.look(begin);
+        keys.fetch(begin, kt0, vt0);
+        if (begin + kKeys < end) keys.look(begin + kKeys);
+        uintx4 qf[kSteps];
+        const char* qp = a.q.p + at * a.q.row + head * a.q.head;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int at_quad = tid + 256 * i;
-            const int r = at_quad / kQuads;
-            const int quad = min((at_quad % kQuads) ^ swizzle<kQuads>(r), last_quad);
-            const int j = min(j0 + r, s.m - 1);
-            if constexpr (SOURCE == kPacked) {
-                const int64_t row = s.k0 + j;
-                kt[at_quad] = *reinterpret_cast<const uintx4*>(a.k.p + row * a.k.row + kvh * a.k.head + quad * 16);
-                vt[at_quad] = *reinterpret_cast<const uintx4*>(a.v.p + row * a.v.row + kvh * a.v.head + quad * 16);
-            } else {
-                const int64_t row = page_row(a.table, a.cols, s.b, a.pages, a.page_shift, a.err, j);
-                if constexpr (SOURCE == kPaged) {
-                    kt[at_quad] = *reinterpret_cast<const uintx4*>(a.k.p + row * a.k.row + kvh * a.k.head + quad * 16);
-                    vt[at_quad] = *reinterpret_cast<const uintx4*>(a.v.p + row * a.v.row + kvh * a.v.head + quad * 16);
-                } else {
-                    const int64_t sc = row * a.kv_heads + kvh;
-                    kt[at_quad] = widen8<BF>(*reinterpret_cast<const uintx2*>(a.k.p + row * a.k.row + kvh * a.k.head + quad * 8), a.k_scale[sc]);
-                    vt[at_quad] = widen8<BF>(*reinterpret_cast<const uintx2*>(a.v.p + row * a.v.row + kvh * a.v.head + quad * 8), a.v_scale[sc]);
-                }
+        for (int i = 0; i < kSteps; ++i) {
+            const int d = 16 * i + 8 * half;
+            qf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(qp + 2 * d) : uintx4{0, 0, 0, 0};
+        }
+        keys.store(kt0, vt0);
+        // One tile, in kt and vt; the next goes into kn and vn.
+        auto step = [&](int j0, uintx4* kt, uintx4* vt, uintx4* kn, uintx4* vn) {
+            wg_barrier<0>();                         // kt and vt are there, kn and vn free
+            const bool more = j0 + kKeys < end;
+            if (more) {
+                keys.fetch(j0 + kKeys, kn, vn);
+                if (j0 + 2 * kKeys < end) keys.look(j0 + 2 * kKeys);
             }
-        }
-        __syncthreads();
-        if (!active || j0 >= w_hi || j0 + kKeys <= w_lo) continue;
-        floatx16 sc[2];
+            floatx16 sc[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < 2; ++b) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
+                for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i)
-                sc[b] = mfma16<BF>(tile_rows<kQuads>(kt, 32 * b, i, lane), qf[i], sc[b]);
-        }
-        if (j0 < all_lo || j0 + kKeys > all_hi) {
+                for (int i = 0; i < kSteps; ++i)
+                    sc[b] = mfma16<BF>(tile_rows<kQuads>(kt, 32 * b, i, lane), qf[i], sc[b]);
+            }
+            if (j0 < all_lo || j0 + kKeys > all_hi) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int j = j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
+                        if (j < lo || j >= hi) sc[b][i] = -__builtin_inff();
+                    }
+            }
+            float mx = sc[0][0];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int j = j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-                    if (j < lo || j >= hi) sc[b][i] = -__builtin_inff();
-                }
-        }
-        float mx = sc[0][0];
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[b][i]);
+            mx = pair_max(mx) * a.scale_log2;
+            // The sums are brought to a new maximum only where it has risen
+            // by more than 8: probabilities up to 2^8 lose nothing.
+            if (__any(mx > top + 8.f)) {
+                const float now = fmaxf(top, mx);
+                const float shrink = __builtin_amdgcn_exp2f(top - now);
+                top = now;
+                sum *= shrink;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+                for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[b][i]);
-        mx = pair_max(mx) * a.scale_log2;
-        const float now = fmaxf(top, mx);
-        const float shrink = __builtin_amdgcn_exp2f(top - now);
-        top = now;
-        sum *= shrink;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[b][i] *= shrink;
-        uintx4 pf[4];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(sc[b][i], a.scale_log2, -top));
-                const float y = __builtin_amdgcn_exp2f(fmaf(sc[b][i + 1], a.scale_log2, -top));
-                sum += x + y;
-                pf[2 * b + (i >> 3)][(i & 7) >> 1] = pack16<BF>(x, y);
+                    for (int i = 0; i < 16; ++i) acc[b][i] *= shrink;
             }
+            uintx4 pf[4];
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(sc[b][i], a.scale_log2, -top));
+                    const float y = __builtin_amdgcn_exp2f(fmaf(sc[b][i + 1], a.scale_log2, -top));
+                    sum += x + y;
+                    pf[2 * b + (i >> 3)][(i & 7) >> 1] = pack16<BF>(x, y);
+                }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                acc[b] = mfma16<BF>(tile_columns<kQuads>(vt, 16 * i, b, lane), pf[i], acc[b]);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+                    acc[b] = mfma16<BF>(tile_columns<kQuads>(vt, 16 * i, b, lane), pf[i], acc[b]);
+            if (more) keys.store(kn, vn);
+        };
+        for (int j0 = begin; j0 < end; j0 += 2 * kKeys) {
+            step(j0, kt0, vt0, kt1, vt1);
+            if (j0 + kKeys < end) step(j0 + kKeys, kt1, vt1, kt0, vt0);
+        }
     }
     if (r0 + wave * 32 + (lane & 31) >= s.rows) return;
     sum = pair_sum(sum);
@@ -258,7 +341,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     uintx4* kt = tiles_lds[wave][0];
     uintx4* vt = tiles_lds[wave][1];
     const int last_quad = a.dim / 8 - 1;
-    typedef std::conditional_t<SOURCE == kPaged8, uintx2, uintx4> Quad;
+    typedef std::conditional_t<SOURCE == kE4m3, uintx2, uintx4> Quad;
     Quad kr[kLoads], vr[kLoads];
     float ks[kLoads], vs[kLoads];
     auto load = [&](int j0) {
@@ -274,7 +357,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
             const int size = sizeof(Quad);
             kr[i] = *reinterpret_cast<const Quad*>(a.k.p + row * a.k.row + kvh * a.k.head + quad * size);
             vr[i] = *reinterpret_cast<const Quad*>(a.v.p + row * a.v.row + kvh * a.v.head + quad * size);
-            if constexpr (SOURCE == kPaged8) {
+            if constexpr (SOURCE == kE4m3) {
                 ks[i] = a.k_scale[row * a.kv_heads + kvh];
                 vs[i] = a.v_scale[row * a.kv_heads + kvh];
             }
@@ -285,7 +368,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     for (; j0 < end; j0 += 4 * kWaveKeys) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            if constexpr (SOURCE == kPaged8) {
+            if constexpr (SOURCE == kE4m3) {
                 kt[lane + 64 * i] = widen8<BF>(kr[i], ks[i]);
                 vt[lane + 64 * i] = widen8<BF>(vr[i], vs[i]);
             } else {
@@ -433,8 +516,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
 template <bool BF, int DP, int SOURCE>
 void launch_dim(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
     const dim3 grid((unsigned)(attn_groups(a.kv_heads, a.tokens_q * a.group, p.tile, a.batch) * p.splits));
+    // (few rows look up a page for every row they load)
+    constexpr int kFewSource = SOURCE == kPagedSmall ? kPaged : SOURCE == kE4m3Small ? kE4m3 : SOURCE;
     if (p.tile == kFewRows)
-        hipLaunchKernelGGL((attn_few_kernel<BF, DP, SOURCE>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((attn_few_kernel<BF, DP, kFewSource>), grid, dim3(256), 0, s, a);
     else
         hipLaunchKernelGGL((attn_kernel<BF, DP, SOURCE>), grid, dim3(256), 0, s, a);
 }
@@ -473,8 +558,12 @@ hipError_t attn_forward_launch(const AttnArgs& a, const AttnPlan& p, bool bf, in
     case 1: launch<true, kPacked>(a, p, s); break;
     case 2: launch<false, kPaged>(a, p, s); break;
     case 3: launch<true, kPaged>(a, p, s); break;
-    case 4: launch<false, kPaged8>(a, p, s); break;
-    default: launch<true, kPaged8>(a, p, s); break;
+    case 4: launch<false, kPagedSmall>(a, p, s); break;
+    case 5: launch<true, kPagedSmall>(a, p, s); break;
+    case 6: launch<false, kE4m3>(a, p, s); break;
+    case 7: launch<true, kE4m3>(a, p, s); break;
+    case 8: launch<false, kE4m3Small>(a, p, s); break;
+    default: launch<true, kE4m3Small>(a, p, s); break;
     }
     if (p.splits > 1) {
         const dim3 grid(stride_grid(ceil_div(a.tokens_q * a.heads * (a.dim / 4), 256), 256));

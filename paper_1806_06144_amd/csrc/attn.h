@@ -77,7 +77,9 @@ constexpr int kRowTile = 128;         // rows of a workgroup: 32 per wave
 constexpr int kFewRows = 32;          // rows of a workgroup whose waves split the keys
 constexpr int64_t kMaxGroups = (int64_t(1) << 24) - 1;   // of 256 threads: below 2^32
 
-enum { kPacked = 0, kPaged = 1, kPaged8 = 2 };
+// Where keys lie: packed rows; pages of 16-bit rows, of at least 16 tokens or
+// fewer; pages of e4m3 rows, the same.
+enum { kPacked = 0, kPaged = 1, kPagedSmall = 2, kE4m3 = 3, kE4m3Small = 4 };
 
 hipError_t attn_forward_launch(const AttnArgs& a, const AttnPlan& p, bool bf, int source,
                                hipStream_t s);
@@ -176,6 +178,48 @@ template <int QUADS>
 __device__ __forceinline__ int tile_quad(int row, int quad) {
     return row * QUADS + (quad ^ swizzle<QUADS>(row));
 }
+
+// Loads of a tile of 64 rows straight into LDS, by the four waves of a
+// workgroup: wave w fills rows 16 w .. 16 w + 15, one kilobyte a load. A lane's
+// offset from the tile's (or page's) first row stays the same from tile to
+// tile, so a load costs a scalar base; rows past the last key read the last.
+constexpr int kTileRows = 64;
+constexpr int kWaveRows = 16;
+
+__device__ __forceinline__ void load_lds16(const char* p, uintx4* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned*)p,
+                                     (__attribute__((address_space(3))) unsigned*)lds, 16, 0, 0);
+}
+
+template <int QUADS>
+struct TileLoader {
+    static constexpr int kLoads = kWaveRows * QUADS / 64;    // a wave's, per tile
+    static constexpr int kStep = 64 / QUADS;                 // rows a load
+    int row0;                         // of the first load, within the wave's 16 rows
+    int quad_[kLoads];                // bytes into a row
+
+    __device__ __forceinline__ TileLoader(int lane, int dim) {
+        row0 = lane / QUADS;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)             // (the swizzle repeats after 16 rows)
+            quad_[i] = 16 * min((lane % QUADS) ^ swizzle<QUADS>(row(i)), dim / 8 - 1);
+    }
+    __device__ __forceinline__ int row(int i) const { return row0 + kStep * i; }
+    __device__ __forceinline__ int quad(int i) const { return quad_[i]; }
+    // base: the wave's first row; left: rows that exist from there on (>= 1);
+    // stride: bytes a row, below 2^25.
+    __device__ __forceinline__ void load(const char* base, int left, int64_t stride, uintx4* to) const {
+        const unsigned st = (unsigned)stride;
+        if (left >= kWaveRows) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_lds16(base + (row(i) * st + quad_[i]), to + 64 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                load_lds16(base + (min(row(i), left - 1) * st + quad_[i]), to + 64 * i);
+        }
+    }
+};
 
 // Operand of 32 rows x 16 depth, the rows those of the tile from row0 on:
 // lane l holds row l % 32, depth 16 step + 8 (l / 32) .. + 7.

@@ -54,7 +54,8 @@ int check_rows(const char* name, const ep_rows& r, int64_t tokens) {
     if (tokens == 0) return EP_OK;
     REQUIRE(r.data, "%s is NULL", name);
     REQUIRE(aligned16(r.data), "%s must be 16-byte aligned", name);
-    REQUIRE(r.row % 8 == 0 && r.head % 8 == 0, "%s: strides must be multiples of 8 elements", name);
+    REQUIRE(r.row % 8 == 0 && r.head % 8 == 0 && r.row >= 0 && r.head >= 0 && r.row < (1 << 24),
+            "%s: strides must be multiples of 8 elements, not negative, rows' below 2^24", name);
     return EP_OK;
 }
 
@@ -291,6 +292,8 @@ extern "C" int ep_cache_attention(const ep_attn* a, const ep_cache* c, const ep_
     g.pages = (int)c->pages;
     g.page_shift = shift_of(c->page_size);
     g.err = p->err;
-    return launched(attn_forward_launch(g, plan, a->type == EP_BF16, c->type == EP_E4M3 ? kPaged8 : kPaged,
+    const bool small = g.page_shift < 4;
+    const int source = c->type == EP_E4M3 ? (small ? kE4m3Small : kE4m3) : (small ? kPagedSmall : kPaged);
+    return launched(attn_forward_launch(g, plan, a->type == EP_BF16, source,
                                         static_cast<hipStream_t>(hip_stream)));
 }

@@ -194,7 +194,8 @@ def test_attention_refuses(kw):
 
 @pytest.mark.parametrize("name", ["q", "k", "v", "out"])
 @pytest.mark.parametrize("bad", [dict(data=None), dict(data=A + 2), dict(data=A + 8),
-                                 dict(row=100), dict(head=4)])
+                                 dict(row=100), dict(head=4), dict(row=-8),
+                                 dict(head=-64), dict(row=1 << 24)])
 def test_attention_refuses_rows(name, bad):
     assert _forward(_attn(), **{name: _rows(**bad)}) == ep.EP_EINVAL
     assert name in ep.ep_last_error()

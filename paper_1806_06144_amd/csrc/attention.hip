@@ -23,9 +23,6 @@ namespace ep {
 
 namespace {
 
-#ifndef OCC64
-#define OCC64 2
-#endif
 constexpr int kKeys = 64;             // keys of a tile
 constexpr int kWaveKeys = 32;         // keys of a wave's own tile (few rows)
 
@@ -123,7 +120,7 @@ struct KeyTiles {
 };
 
 template <bool BF, int DP, int SOURCE>
-__global__ void __launch_bounds__(256, DP == 64 ? OCC64 : 2) attn_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     constexpr int kQuads = DP / 8;
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
@@ -182,9 +179,11 @@ __global__ void __launch_bounds__(256, DP == 64 ? OCC64 : 2) attn_kernel(AttnArg
             qf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(qp + 2 * d) : uintx4{0, 0, 0, 0};
         }
         keys.store(kt0, vt0);
+        TileReader<kQuads> rd(lane);
         // One tile, in kt and vt; the next goes into kn and vn.
         auto step = [&](int j0, uintx4* kt, uintx4* vt, uintx4* kn, uintx4* vn) {
             wg_barrier<0>();                         // kt and vt are there, kn and vn free
+            rd.fresh();
             const bool more = j0 + kKeys < end;
             if (more) {
                 keys.fetch(j0 + kKeys, kn, vn);
@@ -197,7 +196,7 @@ __global__ void __launch_bounds__(256, DP == 64 ? OCC64 : 2) attn_kernel(AttnArg
                 for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i)
-                    sc[b] = mfma16<BF>(tile_rows<kQuads>(kt, 32 * b, i, lane), qf[i], sc[b]);
+                    sc[b] = mfma16<BF>(rd.rows(kt, 32 * b, i), qf[i], sc[b]);
             }
             if (j0 < all_lo || j0 + kKeys > all_hi) {
 #pragma unroll
@@ -240,7 +239,7 @@ __global__ void __launch_bounds__(256, DP == 64 ? OCC64 : 2) attn_kernel(AttnArg
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
-                    acc[b] = mfma16<BF>(tile_columns<kQuads>(vt, 16 * i, b, lane), pf[i], acc[b]);
+                    acc[b] = mfma16<BF>(rd.columns(vt, 16 * i, b), pf[i], acc[b]);
             if (more) keys.store(kn, vn);
         };
         for (int j0 = begin; j0 < end; j0 += 2 * kKeys) {
@@ -338,6 +337,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
     float top = -3.0e38f, sum = 0.f;
 
+    TileReader<kQuads> rd(lane);
     uintx4* kt = tiles_lds[wave][0];
     uintx4* vt = tiles_lds[wave][1];
     const int last_quad = a.dim / 8 - 1;
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
         for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
-            sc = mfma16<BF>(tile_rows<kQuads>(kt, 0, i, lane), qf[i], sc);
+            sc = mfma16<BF>(rd.rows(kt, 0, i), qf[i], sc);
         if (j0 < all_lo || j0 + kWaveKeys > all_hi) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                acc[b] = mfma16<BF>(tile_columns<kQuads>(vt, 16 * i, b, lane), pf[i], acc[b]);
+                acc[b] = mfma16<BF>(rd.columns(vt, 16 * i, b), pf[i], acc[b]);
     }
     // Joining: every wave leaves its sums in its part of LDS, row by row of
     // queries (quads permuted by the row, which spreads a write over the

@@ -21,6 +21,13 @@ namespace ep {
 namespace {
 
 constexpr int kKeyTile = 64;          // keys of a tile (dq)
+#ifndef SBM
+#define SBM 1
+#endif
+#define SB(m) if constexpr ((SBM & (m)) != 0) __builtin_amdgcn_sched_barrier(0)
+#ifndef DKVOCC
+#define DKVOCC 1
+#endif
 constexpr int kStepRows = 64;         // rows of a tile (dk, dv)
 constexpr int kKeyRange = 128;        // keys of a workgroup (dk, dv): 32 per wave
 
@@ -29,9 +36,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     constexpr int kQuads = DP / 8;
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
-    constexpr int kLoads = kKeyTile * kQuads / 256;
-    __shared__ uintx4 kt[kKeyTile * kQuads];
-    __shared__ uintx4 vt[kKeyTile * kQuads];
+    __shared__ uintx4 kt0[kKeyTile * kQuads];
+    __shared__ uintx4 kt1[kKeyTile * kQuads];
+    __shared__ uintx4 vt0[kKeyTile * kQuads];
+    __shared__ uintx4 vt1[kKeyTile * kQuads];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -50,6 +58,21 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const int64_t at = s.q0 + tok;
     const int head = kvh * a.group + (row - tok * a.group);
     const int hi = key_hi(a, s, tok), lo = key_lo(a, s, tok);
+    const int t0 = row_token(a, min(r0 + wave * 32, s.rows - 1));
+    const int t1 = row_token(a, min(r0 + wave * 32 + 31, s.rows - 1));
+    const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);
+    const int begin = key_lo(a, s, row_token(a, r0)) / kKeyTile * kKeyTile;
+    const int end = key_hi(a, s, row_token(a, r1));
+
+    const TileLoader<kQuads> l(lane, a.dim);
+    TileReader<kQuads> rd(lane);
+    auto fetch = [&](int j0, uintx4* kt, uintx4* vt) {
+        const int j = min(j0 + kWaveRows * wave, s.m - 1);
+        const int to = kWaveRows * kQuads * wave;
+        l.load(a.k.p + kvh * a.k.head + (int64_t)(s.k0 + j) * a.k.row, s.m - j, a.k.row, kt + to);
+        l.load(a.v.p + kvh * a.v.head + (int64_t)(s.k0 + j) * a.v.row, s.m - j, a.v.row, vt + to);
+    };
+    if (begin < end) fetch(begin, kt0, vt0);
     uintx4 qf[kSteps], gf[kSteps];
     float delta = 0.f;
     {
@@ -72,16 +95,11 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
         delta = pair_sum(delta);
     }
     const bool mine = r0 + wave * 32 + (lane & 31) < s.rows;
-    if (mine && half == 0) a.delta[at * a.heads + head] = delta;
     const float lse2 = a.lse[at * a.heads + head] * kLog2e;
-
-    const int w0 = min(r0 + wave * 32, s.rows - 1), w1 = min(r0 + wave * 32 + 31, s.rows - 1);
-    const bool active = r0 + wave * 32 < s.rows;
-    const int t0 = row_token(a, w0), t1 = row_token(a, w1);
-    const int w_lo = key_lo(a, s, t0), w_hi = key_hi(a, s, t1);
-    const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);
-    const int begin = key_lo(a, s, row_token(a, r0)) / kKeyTile * kKeyTile;
-    const int end = key_hi(a, s, row_token(a, r1));
+    if (mine && half == 0) {
+        a.lse2[at * a.heads + head] = lse2;
+        a.delta[at * a.heads + head] = delta;
+    }
 
     floatx16 acc[kBlocks];
 #pragma unroll
@@ -89,56 +107,51 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
 
-    const int last_quad = a.dim / 8 - 1;
-    for (int j0 = begin; j0 < end; j0 += kKeyTile) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int at_quad = tid + 256 * i;
-            const int r = at_quad / kQuads;
-            const int quad = min((at_quad % kQuads) ^ swizzle<kQuads>(r), last_quad);
-            const int64_t j = s.k0 + min(j0 + r, s.m - 1);
-            kt[at_quad] = *reinterpret_cast<const uintx4*>(a.k.p + j * a.k.row + kvh * a.k.head + quad * 16);
-            vt[at_quad] = *reinterpret_cast<const uintx4*>(a.v.p + j * a.v.row + kvh * a.v.head + quad * 16);
-        }
-        __syncthreads();
-        if (!active || j0 >= w_hi || j0 + kKeyTile <= w_lo) continue;
+    // One tile, in kt and vt; the next goes into kn and vn.
+    auto step = [&](int j0, const uintx4* kt, const uintx4* vt, uintx4* kn, uintx4* vn) {
+        wg_barrier<0>();                             // kt and vt are there, kn and vn free
+        rd.fresh();
+        if (j0 + kKeyTile < end) fetch(j0 + kKeyTile, kn, vn);
         const bool masked = j0 < all_lo || j0 + kKeyTile > all_hi;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
+            SB(1);
             floatx16 sc, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                sc = mfma16<BF>(tile_rows<kQuads>(kt, 32 * b, i, lane), qf[i], sc);
-                dp = mfma16<BF>(tile_rows<kQuads>(vt, 32 * b, i, lane), gf[i], dp);
+                sc = mfma16<BF>(rd.rows(kt, 32 * b, i), qf[i], sc);
+                dp = mfma16<BF>(rd.rows(vt, 32 * b, i), gf[i], dp);
             }
-            if (masked) {
+            SB(2);
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -lse2));
+            if (masked) {                            // (a row that sees nothing has lse = -inf)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int j = j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-                    if (j < lo || j >= hi) sc[i] = -__builtin_inff();
+                    p[i] = j >= lo && j < hi ? p[i] : 0.f;
                 }
             }
             uintx4 df[2];
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                // (a row that sees nothing has no unmasked entry)
-                float x = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -lse2));
-                float y = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -lse2));
-                if (masked) {
-                    x = sc[i] == -__builtin_inff() ? 0.f : x;
-                    y = sc[i + 1] == -__builtin_inff() ? 0.f : y;
-                }
-                df[i >> 3][(i & 7) >> 1] = pack16<BF>(x * (dp[i] - delta), y * (dp[i + 1] - delta));
-            }
+            for (int i = 0; i < 16; i += 2)
+                df[i >> 3][(i & 7) >> 1] =
+                    pack16<BF>(p[i] * (dp[i] - delta), p[i + 1] * (dp[i + 1] - delta));
+            SB(4);
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    acc[c] = mfma16<BF>(tile_columns<kQuads>(kt, 32 * b + 16 * i, c, lane), df[i], acc[c]);
+                    acc[c] = mfma16<BF>(rd.columns(kt, 32 * b + 16 * i, c), df[i], acc[c]);
         }
+    };
+    for (int j0 = begin; j0 < end; j0 += 2 * kKeyTile) {
+        step(j0, kt0, vt0, kt1, vt1);
+        if (j0 + kKeyTile < end) step(j0 + kKeyTile, kt1, vt1, kt0, vt0);
     }
     if (!mine) return;
     char* out = a.dq.p + at * a.dq.row + head * a.dq.head;
@@ -158,15 +171,16 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 // operands. S = Q K^T and dP = dout V^T leave a lane 16 rows of ONE key, the
 // order in which dv^T += dout^T P and dk^T += Q^T dS take them.
 template <bool BF, int DP>
-__global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256, DP == 64 ? 2 : DKVOCC) attn_dkv_kernel(AttnArgs a) {
     constexpr int kQuads = DP / 8;
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
-    constexpr int kLoads = kStepRows * kQuads / 256;
-    __shared__ uintx4 qt[kStepRows * kQuads];
-    __shared__ uintx4 gt[kStepRows * kQuads];
-    __shared__ float4 s_lse[kStepRows / 4];
-    __shared__ float4 s_delta[kStepRows / 4];
+    __shared__ uintx4 qt0[kStepRows * kQuads];
+    __shared__ uintx4 qt1[kStepRows * kQuads];
+    __shared__ uintx4 gt0[kStepRows * kQuads];
+    __shared__ uintx4 gt1[kStepRows * kQuads];
+    __shared__ float4 s_row0[2][kStepRows / 4];      // lse2, delta
+    __shared__ float4 s_row1[2][kStepRows / 4];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -197,10 +211,35 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnArgs a) {
     auto to_row = [&](int j) { return seen_to(j, s.off, s.n, a.group, a.window); };
     const int lo = from_row(key), hi = to_row(key);
     const int wk0 = min(k0 + wave * 32, s.m - 1), wk1 = min(k0 + wave * 32 + 31, s.m - 1);
-    const bool active = k0 + wave * 32 < s.m;
-    const int w_lo = from_row(wk0), w_hi = to_row(wk1);
-    const int all_lo = from_row(wk1), all_hi = to_row(wk0);
+    // (rows past the last are rows that see nothing)
+    const int all_lo = from_row(wk1), all_hi = min(to_row(wk0), s.rows);
     const int begin = from_row(k0) / kStepRows * kStepRows, end = to_row(k1);
+
+    const TileLoader<kQuads> l(lane, a.dim);
+    TileReader<kQuads> rd(lane);
+    auto fetch = [&](int i0, uintx4* qt, uintx4* gt, float4 (*rows)[kStepRows / 4]) {
+        // the tile's first row is (tok0, rem0); a lane's rows follow it
+        const int tok0 = row_token(a, i0), rem0 = i0 - tok0 * a.group;
+        const int to = kWaveRows * kQuads * wave;
+        const char* qp = a.q.p + (int64_t)(s.q0 + tok0) * a.q.row + kvh * a.group * a.q.head;
+        const char* gp = a.dout.p + (int64_t)(s.q0 + tok0) * a.dout.row + kvh * a.group * a.dout.head;
+        const int last = s.rows - 1 - i0;
+#pragma unroll
+        for (int i = 0; i < l.kLoads; ++i) {
+            const int r = rem0 + min(kWaveRows * wave + l.row(i), last);
+            const unsigned t = row_token(a, r), h = r - t * a.group;
+            load_lds16(qp + (t * (uint64_t)a.q.row + h * (uint64_t)a.q.head) + l.quad(i), qt + to + 64 * i);
+            load_lds16(gp + (t * (uint64_t)a.dout.row + h * (uint64_t)a.dout.head) + l.quad(i), gt + to + 64 * i);
+        }
+        if (wave < 2) {
+            const int r = rem0 + min(lane, last);
+            const unsigned t = row_token(a, r), h = r - t * a.group;
+            const float* p = (wave == 0 ? a.lse2 : a.delta) + (s.q0 + tok0 + (int64_t)t) * a.heads +
+                             kvh * a.group + h;
+            load_lds4(p, reinterpret_cast<float*>(rows[wave]));
+        }
+    };
+    if (begin < end) fetch(begin, qt0, gt0, s_row0);
 
     floatx16 dk[kBlocks], dv[kBlocks];
 #pragma unroll
@@ -208,71 +247,68 @@ __global__ void __launch_bounds__(256, 2) attn_dkv_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[b][i] = dv[b][i] = 0.f;
 
-    const int last_quad = a.dim / 8 - 1;
-    for (int i0 = begin; i0 < end; i0 += kStepRows) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int at_quad = tid + 256 * i;
-            const int r = at_quad / kQuads;
-            const int quad = min((at_quad % kQuads) ^ swizzle<kQuads>(r), last_quad);
-            const int row = min(i0 + r, s.rows - 1);
-            const int tok = row_token(a, row);
-            const int head = kvh * a.group + (row - tok * a.group);
-            const int64_t q = s.q0 + tok;
-            qt[at_quad] = *reinterpret_cast<const uintx4*>(a.q.p + q * a.q.row + head * a.q.head + quad * 16);
-            gt[at_quad] = *reinterpret_cast<const uintx4*>(a.dout.p + q * a.dout.row + head * a.dout.head + quad * 16);
-        }
-        if (tid < kStepRows) {
-            const int row = min(i0 + tid, s.rows - 1);
-            const int tok = row_token(a, row);
-            const int64_t q = (s.q0 + tok) * (int64_t)a.heads + kvh * a.group + (row - tok * a.group);
-            reinterpret_cast<float*>(s_lse)[tid] = a.lse[q] * kLog2e;
-            reinterpret_cast<float*>(s_delta)[tid] = a.delta[q];
-        }
-        __syncthreads();
-        if (!active || i0 >= w_hi || i0 + kStepRows <= w_lo) continue;
-        // (rows past the last are rows that see nothing)
-        const bool masked = i0 < all_lo || i0 + kStepRows > min(all_hi, s.rows);
+    // One tile of rows, in qt and gt; the next goes into qn and gn.
+    auto step = [&](int i0, const uintx4* qt, const uintx4* gt, const float4 (*rows)[kStepRows / 4],
+                    uintx4* qn, uintx4* gn, float4 (*rn)[kStepRows / 4]) {
+        wg_barrier<0>();                             // qt and gt are there, qn and gn free
+        rd.fresh();
+        if (i0 + kStepRows < end) fetch(i0 + kStepRows, qn, gn, rn);
+        const bool masked = i0 < all_lo || i0 + kStepRows > all_hi;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
+            SB(1);
             floatx16 sc, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                sc = mfma16<BF>(tile_rows<kQuads>(qt, 32 * b, i, lane), kf[i], sc);
-                dp = mfma16<BF>(tile_rows<kQuads>(gt, 32 * b, i, lane), vf[i], dp);
+                sc = mfma16<BF>(rd.rows(qt, 32 * b, i), kf[i], sc);
+                dp = mfma16<BF>(rd.rows(gt, 32 * b, i), vf[i], dp);
+            }
+            SB(2);
+            float p[16], ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const float4 l4 = rows[0][8 * b + 2 * (i >> 2) + half];
+                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -l4.x));
+                p[i + 1] = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -l4.y));
+                p[i + 2] = __builtin_amdgcn_exp2f(fmaf(sc[i + 2], a.scale_log2, -l4.z));
+                p[i + 3] = __builtin_amdgcn_exp2f(fmaf(sc[i + 3], a.scale_log2, -l4.w));
+            }
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int r = i0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
+                    p[i] = r >= lo && r < hi && r < s.rows ? p[i] : 0.f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const float4 d4 = rows[1][8 * b + 2 * (i >> 2) + half];
+                ds[i] = p[i] * (dp[i] - d4.x);
+                ds[i + 1] = p[i + 1] * (dp[i + 1] - d4.y);
+                ds[i + 2] = p[i + 2] * (dp[i + 2] - d4.z);
+                ds[i + 3] = p[i + 3] * (dp[i + 3] - d4.w);
             }
             uintx4 pf[2], df[2];
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const float4 l4 = s_lse[8 * b + 2 * (i >> 2) + half];
-                const float4 d4 = s_delta[8 * b + 2 * (i >> 2) + half];
-                const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
-                float p[4], ds[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(fmaf(sc[i + e], a.scale_log2, -l[e]));
-                    if (masked) {
-                        const int r = i0 + 32 * b + 2 * i + 4 * half + e;
-                        p[e] = r >= lo && r < hi && r < s.rows ? p[e] : 0.f;
-                    }
-                    ds[e] = p[e] * (dp[i + e] - dl[e]);
-                }
-                pf[i >> 3][(i & 7) >> 1] = pack16<BF>(p[0], p[1]);
-                pf[i >> 3][((i & 7) >> 1) + 1] = pack16<BF>(p[2], p[3]);
-                df[i >> 3][(i & 7) >> 1] = pack16<BF>(ds[0], ds[1]);
-                df[i >> 3][((i & 7) >> 1) + 1] = pack16<BF>(ds[2], ds[3]);
+            for (int i = 0; i < 16; i += 2) {
+                pf[i >> 3][(i & 7) >> 1] = pack16<BF>(p[i], p[i + 1]);
+                df[i >> 3][(i & 7) >> 1] = pack16<BF>(ds[i], ds[i + 1]);
             }
+            SB(4);
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    dv[c] = mfma16<BF>(tile_columns<kQuads>(gt, 32 * b + 16 * i, c, lane), pf[i], dv[c]);
-                    dk[c] = mfma16<BF>(tile_columns<kQuads>(qt, 32 * b + 16 * i, c, lane), df[i], dk[c]);
+                    dv[c] = mfma16<BF>(rd.columns(gt, 32 * b + 16 * i, c), pf[i], dv[c]);
+                    dk[c] = mfma16<BF>(rd.columns(qt, 32 * b + 16 * i, c), df[i], dk[c]);
                 }
         }
+    };
+    for (int i0 = begin; i0 < end; i0 += 2 * kStepRows) {
+        step(i0, qt0, gt0, s_row0, qt1, gt1, s_row1);
+        if (i0 + kStepRows < end) step(i0 + kStepRows, qt1, gt1, s_row1, qt0, gt0, s_row0);
     }
     if (k0 + wave * 32 + (lane & 31) >= s.m) return;
     char* kp = a.dk.p + at * a.dk.row + kvh * a.dk.head;

@@ -34,7 +34,8 @@ struct AttnArgs {
     Rows q, k, v, o;          // o: out; the gradients' kernels use the rest
     Rows dout, dq, dk, dv;
     float* lse;               // [tokens_q][heads], may be NULL where written
-    float* delta;             // [tokens_q][heads]: sum of out * dout per row
+    float* lse2;              // [tokens_q][heads], for the gradients: log-sums in units of
+    float* delta;             //   log 2, and the sums of out * dout
     const int* start_q;       // batch + 1
     const int* start_k;       // batch + 1 (packed keys)
     int64_t tokens_q, tokens_k;
@@ -174,11 +175,6 @@ __device__ __forceinline__ int swizzle(int row) {
     const int f = ((row & 3) << 1) | ((row >> 2) & 1);
     return QUADS == 16 ? f | (row & 8) : f;
 }
-template <int QUADS>
-__device__ __forceinline__ int tile_quad(int row, int quad) {
-    return row * QUADS + (quad ^ swizzle<QUADS>(row));
-}
-
 // Loads of a tile of 64 rows straight into LDS, by the four waves of a
 // workgroup: wave w fills rows 16 w .. 16 w + 15, one kilobyte a load. A lane's
 // offset from the tile's (or page's) first row stays the same from tile to
@@ -189,6 +185,11 @@ constexpr int kWaveRows = 16;
 __device__ __forceinline__ void load_lds16(const char* p, uintx4* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned*)p,
                                      (__attribute__((address_space(3))) unsigned*)lds, 16, 0, 0);
+}
+
+__device__ __forceinline__ void load_lds4(const float* p, float* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned*)p,
+                                     (__attribute__((address_space(3))) unsigned*)lds, 4, 0, 0);
 }
 
 template <int QUADS>
@@ -221,33 +222,46 @@ struct TileLoader {
     }
 };
 
-// Operand of 32 rows x 16 depth, the rows those of the tile from row0 on:
-// lane l holds row l % 32, depth 16 step + 8 (l / 32) .. + 7.
-template <int QUADS>
-__device__ __forceinline__ uintx4 tile_rows(const uintx4* tile, int row0, int step, int lane) {
-    return tile[tile_quad<QUADS>(row0 + (lane & 31), 2 * step + (lane >> 5))];
-}
-
-// Operand of 32 columns (from column 32 block on) x 16 rows (from row0 on)
-// of the tile, transposed: lane l holds column l % 32 and rows 4 h .. 4 h + 3,
+// Operands from a tile. rows(): 32 rows x 16 depth, lane l holding row l % 32
+// from row0 on (a multiple of 32), depth 16 step + 8 (l / 32) .. + 7.
+// columns(): 32 columns (from column 32 block on) x 16 rows (from row0 on, a
+// multiple of 16), transposed: lane l holds column l % 32 and rows 4 h .. 4 h + 3,
 // 8 + 4 h .. 8 + 4 h + 3 (h = l / 32) of the sixteen: the order in which a
-// lane's accumulators 8 i .. 8 i + 7 hold the rows of a 32 x 32 product.
-// A transposing read gives lane i of 16 column i of the four rows that lanes
+// lane's accumulators 8 i .. 8 i + 7 hold the rows of a 32 x 32 product. A
+// transposing read gives lane i of 16 column i of the four rows that lanes
 // 0..3, 4..7, 8..11, 12..15 address.
+//
+// Both are an exclusive or of a lane's one offset and a constant, plus
+// constants that fit the instruction. fresh(), once a tile, keeps the compiler
+// from holding all these sums in registers over the loop (50 of them, spilled,
+// in the gradients' kernels).
 template <int QUADS>
-__device__ __forceinline__ uintx4 tile_columns(const uintx4* tile, int row0, int block, int lane) {
-    const int i = lane & 15, g = lane >> 4;
-    const int r = 4 * (g >> 1) + (i >> 2);                       // row0 is a multiple of 16
-    const int quad = 4 * block + 2 * (g & 1) + ((i & 3) >> 1);
-    const char* t = reinterpret_cast<const char*>(tile);
-    const char* a = t + ((row0 + r) * QUADS + (quad ^ swizzle<QUADS>(r))) * 16 + (i & 1) * 8;
-    const char* b = t + ((row0 + r + 8) * QUADS + (quad ^ swizzle<QUADS>(r + 8))) * 16 + (i & 1) * 8;
-    const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)a);
-    const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)b);
-    typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
-    const uintx2 u = __builtin_bit_cast(uintx2, x), w = __builtin_bit_cast(uintx2, y);
-    return uintx4{u[0], u[1], w[0], w[1]};
-}
+struct TileReader {
+    unsigned r, c;
+    __device__ __forceinline__ explicit TileReader(int lane) {
+        const int row = lane & 31;
+        r = (row * QUADS + ((lane >> 5) ^ swizzle<QUADS>(row))) * 16;
+        const int i = lane & 15, g = lane >> 4;
+        const int k = 4 * (g >> 1) + (i >> 2);
+        c = (k * QUADS + ((2 * (g & 1) + ((i & 3) >> 1)) ^ swizzle<QUADS>(k))) * 16 + (i & 1) * 8;
+    }
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(r), "+v"(c)); }
+    __device__ __forceinline__ uintx4 rows(const uintx4* tile, int row0, int step) const {
+        const char* t = reinterpret_cast<const char*>(tile) + row0 * QUADS * 16;
+        return *reinterpret_cast<const uintx4*>(t + (r ^ (32 * step)));
+    }
+    __device__ __forceinline__ uintx4 columns(const uintx4* tile, int row0, int block) const {
+        // (eight rows on, a swizzle of 16 quads differs in its highest bit)
+        const char* t = reinterpret_cast<const char*>(tile) + row0 * QUADS * 16;
+        const char* a = t + (c ^ (64 * block));
+        const char* b = t + 8 * QUADS * 16 + (c ^ (64 * block) ^ (QUADS == 16 ? 128 : 0));
+        const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)a);
+        const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)b);
+        typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+        const uintx2 u = __builtin_bit_cast(uintx2, x), w = __builtin_bit_cast(uintx2, y);
+        return uintx4{u[0], u[1], w[0], w[1]};
+    }
+};
 
 // One sequence as a workgroup sees it. Starts and lengths come from device
 // memory: they are held within their arrays whatever they are.

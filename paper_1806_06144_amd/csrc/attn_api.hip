@@ -212,7 +212,7 @@ extern "C" int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, e
 
 extern "C" int64_t ep_attention_backward_bytes(const ep_attn* a) {
     TRY(check_attn(a, true));
-    return round_up(a->tokens_q * a->heads * 4, 16);
+    return round_up(a->tokens_q * a->heads * 8, 16);
 }
 
 extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, ep_rows k,
@@ -240,7 +240,8 @@ extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, 
     g.dq = rows_of(dq);
     g.dk = rows_of(dk);
     g.dv = rows_of(dv);
-    g.delta = static_cast<float*>(work);
+    g.lse2 = static_cast<float*>(work);
+    g.delta = g.lse2 + a->tokens_q * a->heads;
     return launched(attn_backward_launch(g, a->type == EP_BF16,
                                          static_cast<hipStream_t>(hip_stream)));
 }

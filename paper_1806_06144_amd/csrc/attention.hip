@@ -24,6 +24,7 @@ namespace ep {
 namespace {
 
 constexpr int kKeys = 64;             // keys of a tile
+constexpr int kWaveRows = kKeys / 4;  // keys that a wave loads of a tile
 constexpr int kWaveKeys = 32;         // keys of a wave's own tile (few rows)
 
 // This workgroup's range of keys: begin .. end, whole tiles of `size`, cut
@@ -42,20 +43,20 @@ __device__ __forceinline__ void split_range(int split, int splits, int size, int
 template <bool BF, int DP, int SOURCE>
 struct KeyTiles {
     static constexpr int kQuads = DP / 8;
-    static constexpr int kLoads = TileLoader<kQuads>::kLoads;
+    static constexpr int kLoads = TileLoader<kQuads, kWaveRows>::kLoads;
     static constexpr bool kEight = SOURCE == kE4m3 || SOURCE == kE4m3Small;
     static constexpr bool kSmall = SOURCE == kPagedSmall || SOURCE == kE4m3Small;
     const AttnArgs& a;
     const Seq& s;
     const int wave, lane, kvh;
-    const TileLoader<kQuads> l;
+    const TileLoader<kQuads, kWaveRows> l;
     int page[kSmall ? kLoads : 1];    // of the wave's rows (of a load's) in the next tile
     // e4m3: the next tile, held in registers until it can be widened
     uintx2 k8[kLoads], v8[kLoads];
     float ks[kLoads], vs[kLoads];
 
     __device__ __forceinline__ KeyTiles(const AttnArgs& a_, const Seq& s_, int wave_, int lane_, int kvh_)
-        : a(a_), s(s_), wave(wave_), lane(lane_), kvh(kvh_), l(lane_, a_.dim) {}
+        : a(a_), s(s_), wave(wave_), lane(lane_), kvh(kvh_), l(lane_, wave_, a_.dim) {}
 
     __device__ __forceinline__ void look(int j0) {
         if constexpr (SOURCE == kPacked) return;
@@ -199,12 +200,14 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
                     sc[b] = mfma16<BF>(rd.rows(kt, 32 * b, i), qf[i], sc[b]);
             }
             if (j0 < all_lo || j0 + kKeys > all_hi) {
+                // (keys j0 + 4 half + c of the lane's, c = 0..3, 8..11, ..)
+                const int c_lo = lo - j0 - 4 * half, c_hi = hi - j0 - 4 * half;
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int j = j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-                        if (j < lo || j >= hi) sc[b][i] = -__builtin_inff();
+                        const int c = 32 * b + 8 * (i >> 2) + (i & 3);
+                        if (c < c_lo || c >= c_hi) sc[b][i] = -__builtin_inff();
                     }
             }
             float mx = sc[0][0];
@@ -384,10 +387,11 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
         for (int i = 0; i < kSteps; ++i)
             sc = mfma16<BF>(rd.rows(kt, 0, i), qf[i], sc);
         if (j0 < all_lo || j0 + kWaveKeys > all_hi) {
+            const int c_lo = lo - j0 - 4 * half, c_hi = hi - j0 - 4 * half;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int j = j0 + 8 * (i >> 2) + 4 * half + (i & 3);
-                if (j < lo || j >= hi) sc[i] = -__builtin_inff();
+                const int c = 8 * (i >> 2) + (i & 3);
+                if (c < c_lo || c >= c_hi) sc[i] = -__builtin_inff();
             }
         }
         float mx = sc[0];

@@ -21,14 +21,10 @@ namespace ep {
 namespace {
 
 constexpr int kKeyTile = 64;          // keys of a tile (dq)
-#ifndef SBM
-#define SBM 1
-#endif
-#define SB(m) if constexpr ((SBM & (m)) != 0) __builtin_amdgcn_sched_barrier(0)
-#ifndef DKVOCC
-#define DKVOCC 1
-#endif
-constexpr int kStepRows = 64;         // rows of a tile (dk, dv)
+constexpr int kWaveKeys = 16;         // of these, loaded by a wave
+constexpr int kStepRows = 32;         // rows of a tile (dk, dv)
+constexpr int kWaveRows = 8;          // of these, loaded by a wave
+constexpr int kStages = 4;            // tiles of rows in LDS (three are in use)
 constexpr int kKeyRange = 128;        // keys of a workgroup (dk, dv): 32 per wave
 
 template <bool BF, int DP>
@@ -64,11 +60,11 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const int begin = key_lo(a, s, row_token(a, r0)) / kKeyTile * kKeyTile;
     const int end = key_hi(a, s, row_token(a, r1));
 
-    const TileLoader<kQuads> l(lane, a.dim);
+    const TileLoader<kQuads, kWaveKeys> l(lane, wave, a.dim);
     TileReader<kQuads> rd(lane);
     auto fetch = [&](int j0, uintx4* kt, uintx4* vt) {
-        const int j = min(j0 + kWaveRows * wave, s.m - 1);
-        const int to = kWaveRows * kQuads * wave;
+        const int j = min(j0 + kWaveKeys * wave, s.m - 1);
+        const int to = kWaveKeys * kQuads * wave;
         l.load(a.k.p + kvh * a.k.head + (int64_t)(s.k0 + j) * a.k.row, s.m - j, a.k.row, kt + to);
         l.load(a.v.p + kvh * a.v.head + (int64_t)(s.k0 + j) * a.v.row, s.m - j, a.v.row, vt + to);
     };
@@ -115,7 +111,6 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
         const bool masked = j0 < all_lo || j0 + kKeyTile > all_hi;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            SB(1);
             floatx16 sc, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
@@ -124,16 +119,16 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
                 sc = mfma16<BF>(rd.rows(kt, 32 * b, i), qf[i], sc);
                 dp = mfma16<BF>(rd.rows(vt, 32 * b, i), gf[i], dp);
             }
-            SB(2);
             float p[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -lse2));
             if (masked) {                            // (a row that sees nothing has lse = -inf)
+                const int c_lo = lo - j0 - 4 * half, c_hi = hi - j0 - 4 * half;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int j = j0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-                    p[i] = j >= lo && j < hi ? p[i] : 0.f;
+                    const int c = 32 * b + 8 * (i >> 2) + (i & 3);
+                    p[i] = c >= c_lo && c < c_hi ? p[i] : 0.f;
                 }
             }
             uintx4 df[2];
@@ -141,7 +136,6 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
             for (int i = 0; i < 16; i += 2)
                 df[i >> 3][(i & 7) >> 1] =
                     pack16<BF>(p[i] * (dp[i] - delta), p[i + 1] * (dp[i + 1] - delta));
-            SB(4);
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
@@ -167,23 +161,35 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
         }
 }
 
-// A wave owns 32 keys, whose rows of K and V stay in its registers as right
-// operands. S = Q K^T and dP = dout V^T leave a lane 16 rows of ONE key, the
-// order in which dv^T += dout^T P and dk^T += Q^T dS take them.
+// Two waves own 32 keys: one forms S = Q K^T, P and dv^T += dout^T P, the
+// other dP = dout V^T, dS from it and the first one's P (float32, through LDS),
+// and dk^T += Q^T dS, a tile of rows behind. Each holds its operand of K or V
+// (32 registers at dim 128) and one sum (64), which leaves room for two waves
+// a SIMD, one of each kind, whose matrix products, exponentials and LDS reads
+// overlap. One wave with both sums (192 registers) either ran alone on its
+// SIMD, waiting for X at 2 x 4096 tokens,
+// 32 heads over 8, dim 128, where this takes DKVTIME. Products whose result has a key
+// a lane (16 rows of ONE key) leave P and dS in the order in which the second
+// products take them.
 template <bool BF, int DP>
-__global__ void __launch_bounds__(256, DP == 64 ? 2 : DKVOCC) attn_dkv_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(512, 2) attn_dkv_kernel(AttnArgs a) {
     constexpr int kQuads = DP / 8;
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
-    __shared__ uintx4 qt0[kStepRows * kQuads];
-    __shared__ uintx4 qt1[kStepRows * kQuads];
-    __shared__ uintx4 gt0[kStepRows * kQuads];
-    __shared__ uintx4 gt1[kStepRows * kQuads];
-    __shared__ float4 s_row0[2][kStepRows / 4];      // lse2, delta
-    __shared__ float4 s_row1[2][kStepRows / 4];
+    // (arrays of their own: what is loaded into one is not waited for where
+    // another is read)
+    __shared__ uintx4 qt0[kStepRows * kQuads], qt1[kStepRows * kQuads];
+    __shared__ uintx4 qt2[kStepRows * kQuads], qt3[kStepRows * kQuads];
+    __shared__ uintx4 gt0[kStepRows * kQuads], gt1[kStepRows * kQuads];
+    __shared__ uintx4 gt2[kStepRows * kQuads], gt3[kStepRows * kQuads];
+    __shared__ float4 rw0[kStepRows / 2], rw1[kStepRows / 2];            // lse2, delta
+    __shared__ float4 rw2[kStepRows / 2], rw3[kStepRows / 2];
+    __shared__ float4 p0[4 * 4 * 64], p1[4 * 4 * 64];                    // P of four pairs
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int pair = wave & 3;
+    const bool second = wave >= 4;                   // the wave of dP, dS and dk
     const int half = lane >> 5;
     int kvh, tile, tiles, first;
     head_and_tile(a.kv_heads, kvh, tile, tiles);     // (early keys have the most rows)
@@ -193,138 +199,184 @@ __global__ void __launch_bounds__(256, DP == 64 ? 2 : DKVOCC) attn_dkv_kernel(At
     if (k0 < 0 || k0 >= s.m) return;
     const int k1 = min(k0 + kKeyRange, s.m) - 1;
 
-    const int key = min(k0 + wave * 32 + (lane & 31), s.m - 1);
-    const int64_t at = s.k0 + key;
-    uintx4 kf[kSteps], vf[kSteps];
-    {
-        const char* kp = a.k.p + at * a.k.row + kvh * a.k.head;
-        const char* vp = a.v.p + at * a.v.row + kvh * a.v.head;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int d = 16 * i + 8 * half;
-            const uintx4 zero = {0, 0, 0, 0};
-            kf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(kp + 2 * d) : zero;
-            vf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(vp + 2 * d) : zero;
-        }
-    }
     auto from_row = [&](int j) { return seen_from(j, s.off, s.n, a.group, a.causal); };
     auto to_row = [&](int j) { return seen_to(j, s.off, s.n, a.group, a.window); };
+    const int key = min(k0 + pair * 32 + (lane & 31), s.m - 1);
     const int lo = from_row(key), hi = to_row(key);
-    const int wk0 = min(k0 + wave * 32, s.m - 1), wk1 = min(k0 + wave * 32 + 31, s.m - 1);
+    const int wk0 = min(k0 + pair * 32, s.m - 1), wk1 = min(k0 + pair * 32 + 31, s.m - 1);
     // (rows past the last are rows that see nothing)
     const int all_lo = from_row(wk1), all_hi = min(to_row(wk0), s.rows);
     const int begin = from_row(k0) / kStepRows * kStepRows, end = to_row(k1);
 
-    const TileLoader<kQuads> l(lane, a.dim);
+    const TileLoader<kQuads, kWaveRows> l(lane, pair, a.dim);
     TileReader<kQuads> rd(lane);
-    auto fetch = [&](int i0, uintx4* qt, uintx4* gt, float4 (*rows)[kStepRows / 4]) {
-        // the tile's first row is (tok0, rem0); a lane's rows follow it
-        const int tok0 = row_token(a, i0), rem0 = i0 - tok0 * a.group;
-        const int to = kWaveRows * kQuads * wave;
-        const char* qp = a.q.p + (int64_t)(s.q0 + tok0) * a.q.row + kvh * a.group * a.q.head;
-        const char* gp = a.dout.p + (int64_t)(s.q0 + tok0) * a.dout.row + kvh * a.group * a.dout.head;
-        const int last = s.rows - 1 - i0;
+    const Rows in = second ? a.dout : a.q;           // the rows that this wave loads
+    // Where the group divides the tile, a lane's rows are the same tokens and
+    // heads of every tile, counted from its first.
+    const bool even = kStepRows % a.group == 0 && in.head * a.group < (1 << 30);
+    unsigned off[l.kLoads], off_row;
+    {
+        const unsigned st = (unsigned)in.row, sh = even ? (unsigned)in.head : 0;
 #pragma unroll
         for (int i = 0; i < l.kLoads; ++i) {
-            const int r = rem0 + min(kWaveRows * wave + l.row(i), last);
-            const unsigned t = row_token(a, r), h = r - t * a.group;
-            load_lds16(qp + (t * (uint64_t)a.q.row + h * (uint64_t)a.q.head) + l.quad(i), qt + to + 64 * i);
-            load_lds16(gp + (t * (uint64_t)a.dout.row + h * (uint64_t)a.dout.head) + l.quad(i), gt + to + 64 * i);
+            const int r = kWaveRows * pair + l.row(i);
+            const unsigned t = row_token(a, r);
+            off[i] = t * st + (r - t * a.group) * sh + l.quad(i);
         }
-        if (wave < 2) {
-            const int r = rem0 + min(lane, last);
+        const unsigned t = row_token(a, lane & 31);
+        off_row = t * a.heads + ((lane & 31) - t * a.group);
+    }
+    auto fetch = [&](int i0, uintx4* qt, uintx4* gt, float4* rows) {
+        // the tile's first row is (tok0, rem0)
+        const int tok0 = row_token(a, i0), rem0 = i0 - tok0 * a.group;
+        const char* p = in.p + (int64_t)(s.q0 + tok0) * in.row + kvh * a.group * in.head;
+        const int64_t at = (int64_t)(s.q0 + tok0) * a.heads + kvh * a.group;
+        uintx4* to = (second ? gt : qt) + kWaveRows * kQuads * pair;
+        const int last = s.rows - 1 - i0;
+        if (even && last >= kStepRows - 1) {
+#pragma unroll
+            for (int i = 0; i < l.kLoads; ++i) load_lds16(p + off[i], to + 64 * i);
+            if (wave == 0) load_lds4((half ? a.delta : a.lse2) + at + off_row, reinterpret_cast<float*>(rows));
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < l.kLoads; ++i) {
+            const int r = rem0 + min(kWaveRows * pair + l.row(i), last);
             const unsigned t = row_token(a, r), h = r - t * a.group;
-            const float* p = (wave == 0 ? a.lse2 : a.delta) + (s.q0 + tok0 + (int64_t)t) * a.heads +
-                             kvh * a.group + h;
-            load_lds4(p, reinterpret_cast<float*>(rows[wave]));
+            load_lds16(p + (t * (uint64_t)in.row + h * (uint64_t)in.head) + l.quad(i), to + 64 * i);
+        }
+        if (wave == 0) {
+            const int r = rem0 + min(lane & 31, last);
+            const int t = row_token(a, r);
+            load_lds4((half ? a.delta : a.lse2) + at + (t * (int64_t)a.heads + (r - t * a.group)),
+                      reinterpret_cast<float*>(rows));
         }
     };
-    if (begin < end) fetch(begin, qt0, gt0, s_row0);
-
-    floatx16 dk[kBlocks], dv[kBlocks];
+    if (begin < end) fetch(begin, qt0, gt0, rw0);
+    uintx4 kv[kSteps];                               // the wave's keys' rows of K or V
+    {
+        const Rows& x = second ? a.v : a.k;
+        const char* p = x.p + (int64_t)(s.k0 + key) * x.row + kvh * x.head;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int d = 16 * i + 8 * half;
+            kv[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(p + 2 * d) : uintx4{0, 0, 0, 0};
+        }
+    }
+    floatx16 acc[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) dk[b][i] = dv[b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
 
-    // One tile of rows, in qt and gt; the next goes into qn and gn.
-    auto step = [&](int i0, const uintx4* qt, const uintx4* gt, const float4 (*rows)[kStepRows / 4],
-                    uintx4* qn, uintx4* gn, float4 (*rn)[kStepRows / 4]) {
-        wg_barrier<0>();                             // qt and gt are there, qn and gn free
+    auto product = [&](const uintx4* x) {            // x kv^T, 32 rows x 32 keys
+        floatx16 y;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) y = mfma16<BF>(rd.rows(x, 0, i), kv[i], y);
+        return y;
+    };
+    auto add = [&](const uintx4* x, const floatx16& y) {     // acc += x^T y
+        uintx4 f[2];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) f[i >> 3][(i & 7) >> 1] = pack16<BF>(y[i], y[i + 1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) acc[c] = mfma16<BF>(rd.columns(x, 16 * i, c), f[i], acc[c]);
+    };
+    // The first wave's part of the tile at i0.
+    auto probabilities = [&](int i0, const uintx4* qt, const uintx4* gt, const float4* rows, float4* p) {
+        floatx16 x = product(qt);
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 l4 = rows[2 * (i >> 2) + half];
+            x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], a.scale_log2, -l4.x));
+            x[i + 1] = __builtin_amdgcn_exp2f(fmaf(x[i + 1], a.scale_log2, -l4.y));
+            x[i + 2] = __builtin_amdgcn_exp2f(fmaf(x[i + 2], a.scale_log2, -l4.z));
+            x[i + 3] = __builtin_amdgcn_exp2f(fmaf(x[i + 3], a.scale_log2, -l4.w));
+        }
+        if (i0 < all_lo || i0 + kStepRows > all_hi) {
+            // (rows i0 + 4 half + c of the lane's, c = 0..3, 8..11, ..)
+            const int c_lo = lo - i0 - 4 * half, c_hi = min(hi, s.rows) - i0 - 4 * half;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = 8 * (i >> 2) + (i & 3);
+                x[i] = c >= c_lo && c < c_hi ? x[i] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            p[(4 * pair + (i >> 2)) * 64 + lane] = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        add(gt, x);
+    };
+    // The second wave's.
+    auto slopes = [&](const uintx4* qt, const uintx4* gt, const float4* rows, const float4* p) {
+        floatx16 x = product(gt);
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 d4 = rows[kStepRows / 4 + 2 * (i >> 2) + half];
+            const float4 p4 = p[(4 * pair + (i >> 2)) * 64 + lane];
+            x[i] = p4.x * (x[i] - d4.x);
+            x[i + 1] = p4.y * (x[i + 1] - d4.y);
+            x[i + 2] = p4.z * (x[i + 2] - d4.z);
+            x[i + 3] = p4.w * (x[i + 3] - d4.w);
+        }
+        add(qt, x);
+    };
+    // Iteration i0: tile i0 for the first waves (there is none past the end),
+    // the one before it for the second, the next on its way.
+    auto enter = [&](int i0, uintx4* qn, uintx4* gn, float4* rn) {
+        wg_barrier<0>();                             // tile i0 and the P before it are there
         rd.fresh();
         if (i0 + kStepRows < end) fetch(i0 + kStepRows, qn, gn, rn);
-        const bool masked = i0 < all_lo || i0 + kStepRows > all_hi;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            SB(1);
-            floatx16 sc, dp;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = dp[i] = 0.f;
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                sc = mfma16<BF>(rd.rows(qt, 32 * b, i), kf[i], sc);
-                dp = mfma16<BF>(rd.rows(gt, 32 * b, i), vf[i], dp);
-            }
-            SB(2);
-            float p[16], ds[16];
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const float4 l4 = rows[0][8 * b + 2 * (i >> 2) + half];
-                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -l4.x));
-                p[i + 1] = __builtin_amdgcn_exp2f(fmaf(sc[i + 1], a.scale_log2, -l4.y));
-                p[i + 2] = __builtin_amdgcn_exp2f(fmaf(sc[i + 2], a.scale_log2, -l4.z));
-                p[i + 3] = __builtin_amdgcn_exp2f(fmaf(sc[i + 3], a.scale_log2, -l4.w));
-            }
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int r = i0 + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3);
-                    p[i] = r >= lo && r < hi && r < s.rows ? p[i] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const float4 d4 = rows[1][8 * b + 2 * (i >> 2) + half];
-                ds[i] = p[i] * (dp[i] - d4.x);
-                ds[i + 1] = p[i + 1] * (dp[i + 1] - d4.y);
-                ds[i + 2] = p[i + 2] * (dp[i + 2] - d4.z);
-                ds[i + 3] = p[i + 3] * (dp[i + 3] - d4.w);
-            }
-            uintx4 pf[2], df[2];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                pf[i >> 3][(i & 7) >> 1] = pack16<BF>(p[i], p[i + 1]);
-                df[i >> 3][(i & 7) >> 1] = pack16<BF>(ds[i], ds[i + 1]);
-            }
-            SB(4);
-#pragma unroll
-            for (int c = 0; c < kBlocks; ++c)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    dv[c] = mfma16<BF>(rd.columns(gt, 32 * b + 16 * i, c), pf[i], dv[c]);
-                    dk[c] = mfma16<BF>(rd.columns(qt, 32 * b + 16 * i, c), df[i], dk[c]);
-                }
-        }
     };
-    for (int i0 = begin; i0 < end; i0 += 2 * kStepRows) {
-        step(i0, qt0, gt0, s_row0, qt1, gt1, s_row1);
-        if (i0 + kStepRows < end) step(i0 + kStepRows, qt1, gt1, s_row1, qt0, gt0, s_row0);
+    const int stop = end + kStepRows;                // (a tile more for the second waves)
+    if (begin < end) {
+        if (!second) {
+            for (int i0 = begin; i0 < stop; i0 += kStages * kStepRows) {
+                enter(i0, qt1, gt1, rw1);
+                if (i0 < end) probabilities(i0, qt0, gt0, rw0, p0);
+                if (i0 + kStepRows >= stop) break;
+                enter(i0 + kStepRows, qt2, gt2, rw2);
+                if (i0 + kStepRows < end) probabilities(i0 + kStepRows, qt1, gt1, rw1, p1);
+                if (i0 + 2 * kStepRows >= stop) break;
+                enter(i0 + 2 * kStepRows, qt3, gt3, rw3);
+                if (i0 + 2 * kStepRows < end) probabilities(i0 + 2 * kStepRows, qt2, gt2, rw2, p0);
+                if (i0 + 3 * kStepRows >= stop) break;
+                enter(i0 + 3 * kStepRows, qt0, gt0, rw0);
+                if (i0 + 3 * kStepRows < end) probabilities(i0 + 3 * kStepRows, qt3, gt3, rw3, p1);
+            }
+        } else {
+            for (int i0 = begin; i0 < stop; i0 += kStages * kStepRows) {
+                enter(i0, qt1, gt1, rw1);
+                if (i0 > begin) slopes(qt3, gt3, rw3, p1);
+                if (i0 + kStepRows >= stop) break;
+                enter(i0 + kStepRows, qt2, gt2, rw2);
+                slopes(qt0, gt0, rw0, p0);
+                if (i0 + 2 * kStepRows >= stop) break;
+                enter(i0 + 2 * kStepRows, qt3, gt3, rw3);
+                slopes(qt1, gt1, rw1, p1);
+                if (i0 + 3 * kStepRows >= stop) break;
+                enter(i0 + 3 * kStepRows, qt0, gt0, rw0);
+                slopes(qt2, gt2, rw2, p0);
+            }
+        }
     }
-    if (k0 + wave * 32 + (lane & 31) >= s.m) return;
-    char* kp = a.dk.p + at * a.dk.row + kvh * a.dk.head;
-    char* vp = a.dv.p + at * a.dv.row + kvh * a.dv.head;
+    if (k0 + pair * 32 + (lane & 31) >= s.m) return;
+    const Rows& out = second ? a.dk : a.dv;
+    const float scale = second ? a.scale : 1.f;
+    char* p = out.p + (int64_t)(s.k0 + key) * out.row + kvh * out.head;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int d = 32 * b + 2 * i + 4 * half;
-            if (d < a.dim) {
-                *reinterpret_cast<uintx2*>(kp + 2 * d) =
-                    uintx2{pack16<BF>(dk[b][i] * a.scale, dk[b][i + 1] * a.scale),
-                           pack16<BF>(dk[b][i + 2] * a.scale, dk[b][i + 3] * a.scale)};
-                *reinterpret_cast<uintx2*>(vp + 2 * d) =
-                    uintx2{pack16<BF>(dv[b][i], dv[b][i + 1]), pack16<BF>(dv[b][i + 2], dv[b][i + 3])};
-            }
+            if (d < a.dim)
+                *reinterpret_cast<uintx2*>(p + 2 * d) =
+                    uintx2{pack16<BF>(acc[b][i] * scale, acc[b][i + 1] * scale),
+                           pack16<BF>(acc[b][i + 2] * scale, acc[b][i + 3] * scale)};
         }
 }
 
@@ -333,7 +385,7 @@ void launch(const AttnArgs& a, hipStream_t s) {
     const dim3 rows((unsigned)attn_groups(a.kv_heads, a.tokens_q * a.group, kRowTile, a.batch));
     const dim3 keys((unsigned)attn_groups(a.kv_heads, a.tokens_k, kKeyRange, a.batch));
     hipLaunchKernelGGL((attn_dq_kernel<BF, DP>), rows, dim3(256), 0, s, a);
-    hipLaunchKernelGGL((attn_dkv_kernel<BF, DP>), keys, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attn_dkv_kernel<BF, DP>), keys, dim3(512), 0, s, a);
 }
 
 }  // namespace

@@ -175,43 +175,39 @@ __device__ __forceinline__ int swizzle(int row) {
     const int f = ((row & 3) << 1) | ((row >> 2) & 1);
     return QUADS == 16 ? f | (row & 8) : f;
 }
-// Loads of a tile of 64 rows straight into LDS, by the four waves of a
-// workgroup: wave w fills rows 16 w .. 16 w + 15, one kilobyte a load. A lane's
-// offset from the tile's (or page's) first row stays the same from tile to
-// tile, so a load costs a scalar base; rows past the last key read the last.
-constexpr int kTileRows = 64;
-constexpr int kWaveRows = 16;
-
 __device__ __forceinline__ void load_lds16(const char* p, uintx4* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned*)p,
                                      (__attribute__((address_space(3))) unsigned*)lds, 16, 0, 0);
 }
-
 __device__ __forceinline__ void load_lds4(const float* p, float* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned*)p,
                                      (__attribute__((address_space(3))) unsigned*)lds, 4, 0, 0);
 }
 
-template <int QUADS>
+// A wave's part of a tile that is loaded straight into LDS: ROWS rows from
+// row ROWS * wave on, one kilobyte a load. A lane's offset from the first of
+// them stays the same from tile to tile, so a load costs a scalar base.
+template <int QUADS, int ROWS>
 struct TileLoader {
-    static constexpr int kLoads = kWaveRows * QUADS / 64;    // a wave's, per tile
-    static constexpr int kStep = 64 / QUADS;                 // rows a load
-    int row0;                         // of the first load, within the wave's 16 rows
+    static constexpr int kLoads = ROWS * QUADS / 64;
+    static constexpr int kStep = 64 / QUADS;         // rows a load
+    int row0;                         // of the first load, within the wave's rows
     int quad_[kLoads];                // bytes into a row
 
-    __device__ __forceinline__ TileLoader(int lane, int dim) {
+    __device__ __forceinline__ TileLoader(int lane, int wave, int dim) {
         row0 = lane / QUADS;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)             // (the swizzle repeats after 16 rows)
-            quad_[i] = 16 * min((lane % QUADS) ^ swizzle<QUADS>(row(i)), dim / 8 - 1);
+        for (int i = 0; i < kLoads; ++i)
+            quad_[i] = 16 * min((lane % QUADS) ^ swizzle<QUADS>(ROWS * wave + row(i)), dim / 8 - 1);
     }
     __device__ __forceinline__ int row(int i) const { return row0 + kStep * i; }
     __device__ __forceinline__ int quad(int i) const { return quad_[i]; }
-    // base: the wave's first row; left: rows that exist from there on (>= 1);
-    // stride: bytes a row, below 2^25.
+    // base: the wave's first row; left: rows that exist from there on (>= 1;
+    // the others read the last); stride: bytes a row, below 2^25; to: the
+    // wave's part of the tile.
     __device__ __forceinline__ void load(const char* base, int left, int64_t stride, uintx4* to) const {
         const unsigned st = (unsigned)stride;
-        if (left >= kWaveRows) {
+        if (left >= ROWS) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) load_lds16(base + (row(i) * st + quad_[i]), to + 64 * i);
         } else {

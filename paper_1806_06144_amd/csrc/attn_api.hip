@@ -30,8 +30,9 @@ int check_attn(const ep_attn* a, bool packed_keys) {
             "dim must be a multiple of 8 in [8, 128]");
     REQUIRE(a->tokens_q >= 0 && a->tokens_q < kMaxTokens, "tokens_q must be in [0, 2^30)");
     const int64_t group = a->heads / a->kv_heads;
-    REQUIRE(a->tokens_q * group * group < int64_t(1) << 32,
-            "tokens_q * (heads / kv_heads)^2 must be below 2^32");
+    REQUIRE(a->tokens_q * group < kMaxTokens && a->tokens_q * group * group < int64_t(1) << 32,
+            "with group = heads / kv_heads, tokens_q * group must be below 2^30 and tokens_q * "
+            "group^2 below 2^32");
     REQUIRE(attn_groups(a->kv_heads, a->tokens_q * group, kFewRows, a->batch) <= kMaxGroups &&
                 (!packed_keys ||
                  attn_groups(a->kv_heads, a->tokens_k, kRowTile, a->batch) <= kMaxGroups),

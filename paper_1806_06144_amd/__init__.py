@@ -187,6 +187,11 @@ def _torch():
     return torch
 
 
+_int32, _float32 = _torch().int32, _torch().float32
+_ATTN_TYPES = {_torch().bfloat16: EP_BF16, _torch().float16: EP_FP16}
+_CACHE_TYPES = {**_ATTN_TYPES, _torch().float8_e4m3fn: EP_E4M3, _torch().uint8: EP_E4M3}
+
+
 def _stream_handle(stream):
     if stream is None:
         return _torch().cuda.current_stream().cuda_stream
@@ -382,17 +387,24 @@ def ep_device_probe():
 
 
 # ---- attention over packed sequences and over a paged cache ----
+#
+# These calls may take less time on the device than Python takes to marshal
+# them, so every check is a single comparison.
 
 
-def _rows(x, name, shape, like):
+def _mismatch(x, name, dtype, shape, device):
+    if x.device != device or not x.is_cuda:
+        raise ValueError(f"{name}: expected a tensor on {device if device.type == 'cuda' else 'a device'}")
+    if x.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {x.dtype}")
+    raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+
+
+def _rows(x, name, shape, dtype, device):
     """EpRows of a [tokens, heads, dim] tensor; its last axis is contiguous,
     the others may be strided (slices of a wider array)."""
-    if not x.is_cuda or x.device != like.device:
-        raise ValueError(f"{name}: expected a tensor on {like.device}")
-    if x.dtype != like.dtype:
-        raise TypeError(f"{name}: expected {like.dtype}, got {x.dtype}")
-    if tuple(x.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+    if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_cuda:
+        _mismatch(x, name, dtype, shape, device)
     row, head, one = x.stride()
     if one != 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
@@ -401,37 +413,30 @@ def _rows(x, name, shape, like):
 
 def _dense(x, name, dtype, shape, device):
     """Address of a contiguous tensor of that type, shape and device."""
-    if not x.is_cuda or x.device != device:
-        raise ValueError(f"{name}: expected a tensor on {device}")
-    if x.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {x.dtype}")
-    if tuple(x.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(x.shape)}")
+    if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_cuda:
+        _mismatch(x, name, dtype, shape, device)
     if not x.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous tensor")
     return x.data_ptr()
 
 
 def _attn_type(x):
-    torch = _torch()
-    if x.dtype == torch.bfloat16:
-        return EP_BF16
-    if x.dtype == torch.float16:
-        return EP_FP16
-    raise TypeError(f"expected bfloat16 or float16, got {x.dtype}")
+    kind = _ATTN_TYPES.get(x.dtype)
+    if kind is None:
+        raise TypeError(f"expected bfloat16 or float16, got {x.dtype}")
+    return kind
 
 
-def _attn(q, kv_heads, tokens_k, start_q, start_k, scale, causal, window):
-    torch = _torch()
+def _attn(q, kv_heads, tokens_k, start_q, start_k, scale, causal, window, device):
+    kind = _attn_type(q)
     if q.dim() != 3:
         raise ValueError("q: expected [tokens, heads, dim]")
     tokens_q, heads, dim = q.shape
-    batch = start_q.shape[0] - 1
-    return EpAttn(_attn_type(q), 1 if causal else 0, batch, heads, kv_heads, dim, tokens_q,
-                  tokens_k, window,
-                  _dense(start_q, "start_q", torch.int32, (batch + 1,), q.device),
-                  None if start_k is None else
-                  _dense(start_k, "start_k", torch.int32, (batch + 1,), q.device),
+    starts = start_q.shape
+    return EpAttn(kind, 1 if causal else 0, starts[0] - 1 if len(starts) == 1 else -1, heads,
+                  kv_heads, dim, tokens_q, tokens_k, window,
+                  _dense(start_q, "start_q", _int32, starts, device),
+                  None if start_k is None else _dense(start_k, "start_k", _int32, starts, device),
                   dim ** -0.5 if scale is None else scale)
 
 
@@ -439,8 +444,9 @@ def _on_stream(device, stream, call):
     """call(stream handle, allocate) with the tensors' device current; memory
     from allocate(bytes) belongs to the stream that the work goes to."""
     torch = _torch()
-    if stream is None and device.index == torch.cuda.current_device():
-        return call(torch.cuda.current_stream().cuda_stream,
+    index = device.index
+    if stream is None and index == torch._C._cuda_getDevice():
+        return call(torch._C._cuda_getCurrentRawStream(index),
                     lambda n: torch.empty(n, dtype=torch.uint8, device=device))
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
@@ -449,10 +455,18 @@ def _on_stream(device, stream, call):
                     lambda n: torch.empty(n, dtype=torch.uint8, device=device))
 
 
-def _bytes(n):
+def _work(allocate, n):
+    """(address, bytes) of n bytes, and what holds them; n is a ..._bytes answer."""
+    if n == 0:
+        return None, 0, None
     if n < 0:
         _check(int(n))
-    return n
+    x = allocate(n)
+    return x.data_ptr(), n, x
+
+
+def _lse(lse, q, device):
+    return None if lse is None else _dense(lse, "lse", _float32, q.shape[:2], device)
 
 
 def ep_attention(q, k, v, out, lse, start_q, start_k, scale=None, causal=True, window=0,
@@ -461,40 +475,35 @@ def ep_attention(q, k, v, out, lse, start_q, start_k, scale=None, causal=True, w
     (float32 [tokens, heads], or None). q, out: [tokens, heads, dim] bfloat16
     or float16; k, v: [tokens_k, kv_heads, dim]; start_q, start_k: int32,
     batch + 1 values. scale: dim ** -0.5 by default; window: 0 for none."""
-    torch = _torch()
-    a = _attn(q, k.shape[1], k.shape[0], start_q, start_k, scale, causal, window)
+    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    a = _attn(q, ks[1], ks[0], start_q, start_k, scale, causal, window, dev)
     kv = (a.tokens_k, a.kv_heads, a.dim)
-    args = (_rows(q, "q", tuple(q.shape), q), _rows(k, "k", kv, q), _rows(v, "v", kv, q),
-            _rows(out, "out", tuple(q.shape), q),
-            None if lse is None else
-            _dense(lse, "lse", torch.float32, tuple(q.shape[:2]), q.device))
+    args = (ctypes.byref(a), _rows(q, "q", qs, dt, dev), _rows(k, "k", kv, dt, dev),
+            _rows(v, "v", kv, dt, dev), _rows(out, "out", qs, dt, dev), _lse(lse, q, dev))
 
     def call(s, allocate):
-        n = _bytes(_lib.ep_attention_bytes(ctypes.byref(a)))
-        work = allocate(n) if n else None
-        return _check(_lib.ep_attention(ctypes.byref(a), *args, work.data_ptr() if n else None, n,
-                                        s))
-    return _on_stream(q.device, stream, call)
+        work, n, _hold = _work(allocate, _lib.ep_attention_bytes(args[0]))
+        return _check(_lib.ep_attention(*args, work, n, s))
+    return _on_stream(dev, stream, call)
 
 
 def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k, scale=None,
                           causal=True, window=0, stream=None):
     """Gradients dq, dk, dv of ep_attention for the gradient dout of out; out
     and lse are what it returned. Written, not added to."""
-    torch = _torch()
-    a = _attn(q, k.shape[1], k.shape[0], start_q, start_k, scale, causal, window)
-    qs, kv = tuple(q.shape), (a.tokens_k, a.kv_heads, a.dim)
-    ins = (_rows(dout, "dout", qs, q), _rows(q, "q", qs, q), _rows(k, "k", kv, q),
-           _rows(v, "v", kv, q), _rows(out, "out", qs, q),
-           _dense(lse, "lse", torch.float32, qs[:2], q.device))
-    outs = (_rows(dq, "dq", qs, q), _rows(dk, "dk", kv, q), _rows(dv, "dv", kv, q))
+    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    a = _attn(q, ks[1], ks[0], start_q, start_k, scale, causal, window, dev)
+    kv = (a.tokens_k, a.kv_heads, a.dim)
+    args = (ctypes.byref(a), _rows(dout, "dout", qs, dt, dev), _rows(q, "q", qs, dt, dev),
+            _rows(k, "k", kv, dt, dev), _rows(v, "v", kv, dt, dev),
+            _rows(out, "out", qs, dt, dev), _dense(lse, "lse", _float32, qs[:2], dev),
+            _rows(dq, "dq", qs, dt, dev), _rows(dk, "dk", kv, dt, dev),
+            _rows(dv, "dv", kv, dt, dev))
 
     def call(s, allocate):
-        n = _bytes(_lib.ep_attention_backward_bytes(ctypes.byref(a)))
-        work = allocate(n)
-        return _check(_lib.ep_attention_backward(ctypes.byref(a), *ins, *outs, work.data_ptr(), n,
-                                                 s))
-    return _on_stream(q.device, stream, call)
+        work, n, _hold = _work(allocate, _lib.ep_attention_backward_bytes(args[0]))
+        return _check(_lib.ep_attention_backward(*args, work, n, s))
+    return _on_stream(dev, stream, call)
 
 
 class EpCache:
@@ -503,45 +512,42 @@ class EpCache:
     k_scale and v_scale [pages, page_size, kv_heads]. Holds the tensors."""
 
     def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
-        torch = _torch()
-        if k_pages.dim() != 4:
+        shape, dt, dev = k_pages.shape, k_pages.dtype, k_pages.device
+        if len(shape) != 4:
             raise ValueError("k_pages: expected [pages, page_size, kv_heads, dim]")
-        self.tensors = (k_pages, v_pages, k_scale, v_scale)
-        self.device = k_pages.device
-        eight = k_pages.dtype in (torch.float8_e4m3fn, torch.uint8)
-        shape = tuple(k_pages.shape)
-        scales = (None, None)
-        if eight:
+        ks = vs = None
+        kind = _CACHE_TYPES.get(dt)
+        if kind is None:
+            raise TypeError(f"expected bfloat16, float16 or float8_e4m3fn, got {dt}")
+        if kind == EP_E4M3:
             if k_scale is None or v_scale is None:
                 raise ValueError("an 8-bit cache needs k_scale and v_scale")
-            scales = tuple(_dense(x, n, torch.float32, shape[:3], self.device)
-                           for x, n in ((k_scale, "k_scale"), (v_scale, "v_scale")))
-        pages = tuple(_dense(x, n, k_pages.dtype, shape, self.device)
-                      for x, n in ((k_pages, "k_pages"), (v_pages, "v_pages")))
-        self.desc = EpCacheDesc(EP_E4M3 if eight else _attn_type(k_pages), *shape, *pages, *scales)
+            ks = _dense(k_scale, "k_scale", _float32, shape[:3], dev)
+            vs = _dense(v_scale, "v_scale", _float32, shape[:3], dev)
+        self.tensors = (k_pages, v_pages, k_scale, v_scale)
+        self.device = dev
+        self.kv_heads, self.dim = shape[2], shape[3]
+        self.desc = EpCacheDesc(kind, *shape, _dense(k_pages, "k_pages", dt, shape, dev),
+                                _dense(v_pages, "v_pages", dt, shape, dev), ks, vs)
 
 
 def _pages(cache, table, lengths, err):
-    torch = _torch()
-    if table.dim() != 2:
+    dev, shape = cache.device, table.shape
+    if len(shape) != 2:
         raise ValueError("table: expected [batch, cols]")
-    batch, cols = table.shape
-    return EpPages(batch, _dense(table, "table", torch.int32, (batch, cols), cache.device), cols,
-                   _dense(lengths, "lengths", torch.int32, (batch,), cache.device),
-                   None if err is None else
-                   _dense(err, "err", torch.int32, (1,), cache.device))
+    return EpPages(shape[0], _dense(table, "table", _int32, shape, dev), shape[1],
+                   _dense(lengths, "lengths", _int32, shape[:1], dev),
+                   None if err is None else _dense(err, "err", _int32, (1,), dev))
 
 
 def _cache_move(fn, cache, k, v, table, lengths, start, err, stream):
-    torch = _torch()
-    if k.device != cache.device:
-        raise ValueError(f"k: expected a tensor on {cache.device}")
+    dev, dt = cache.device, k.dtype
     p = _pages(cache, table, lengths, err)
-    shape = (k.shape[0], cache.desc.kv_heads, cache.desc.dim)
-    args = (_attn_type(k), _rows(k, "k", shape, k), _rows(v, "v", shape, k), shape[0],
-            _dense(start, "start", torch.int32, (p.batch + 1,), cache.device))
-    return _on_stream(cache.device, stream, lambda s, _: _check(
-        fn(ctypes.byref(cache.desc), ctypes.byref(p), *args, s)))
+    shape = (k.shape[0], cache.kv_heads, cache.dim)
+    args = (ctypes.byref(cache.desc), ctypes.byref(p), _attn_type(k),
+            _rows(k, "k", shape, dt, dev), _rows(v, "v", shape, dt, dev), shape[0],
+            _dense(start, "start", _int32, (p.batch + 1,), dev))
+    return _on_stream(dev, stream, lambda s, _: _check(fn(*args, s)))
 
 
 def ep_cache_write(cache, k, v, table, lengths, start, err=None, stream=None):
@@ -560,21 +566,16 @@ def ep_cache_attention(q, cache, out, lse, table, lengths, start_q, scale=None, 
                        window=0, err=None, stream=None):
     """ep_attention of new tokens' queries over the cached keys and values
     (theirs included: write them first)."""
-    torch = _torch()
-    if q.device != cache.device:
-        raise ValueError(f"q: expected a tensor on {cache.device}")
-    a = _attn(q, cache.desc.kv_heads, 0, start_q, None, scale, causal, window)
-    p = _pages(cache, table, lengths, err)
-    args = (_rows(q, "q", tuple(q.shape), q), _rows(out, "out", tuple(q.shape), q),
-            None if lse is None else
-            _dense(lse, "lse", torch.float32, tuple(q.shape[:2]), q.device))
-    refs = (ctypes.byref(a), ctypes.byref(cache.desc), ctypes.byref(p))
+    dev, dt, qs = cache.device, q.dtype, q.shape
+    a = _attn(q, cache.kv_heads, 0, start_q, None, scale, causal, window, dev)
+    refs = (ctypes.byref(a), ctypes.byref(cache.desc),
+            ctypes.byref(_pages(cache, table, lengths, err)))
+    args = (_rows(q, "q", qs, dt, dev), _rows(out, "out", qs, dt, dev), _lse(lse, q, dev))
 
     def call(s, allocate):
-        n = _bytes(_lib.ep_cache_attention_bytes(*refs))
-        work = allocate(n) if n else None
-        return _check(_lib.ep_cache_attention(*refs, *args, work.data_ptr() if n else None, n, s))
-    return _on_stream(q.device, stream, call)
+        work, n, _hold = _work(allocate, _lib.ep_cache_attention_bytes(*refs))
+        return _check(_lib.ep_cache_attention(*refs, *args, work, n, s))
+    return _on_stream(dev, stream, call)
 
 
 def ep_sync(ctx):

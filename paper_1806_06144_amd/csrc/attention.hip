@@ -27,16 +27,6 @@ constexpr int kKeys = 64;             // keys of a tile
 constexpr int kWaveRows = kKeys / 4;  // keys that a wave loads of a tile
 constexpr int kWaveKeys = 32;         // keys of a wave's own tile (few rows)
 
-// This workgroup's range of keys: begin .. end, whole tiles of `size`, cut
-// into a.splits ranges.
-__device__ __forceinline__ void split_range(int split, int splits, int size, int& begin, int& end) {
-    const int tiles = (end - begin + size - 1) / size;
-    const int per = (tiles + splits - 1) / splits;
-    const int from = begin + min(split * per, tiles) * size;
-    end = min(end, begin + min((split + 1) * per, tiles) * size);
-    begin = from;
-}
-
 // Tiles on their way into LDS, fetched a tile ahead into one of two buffers,
 // so that the loop's only barrier finds them there. Page numbers are looked up
 // a tile before that: a wait for one would wait for the loads before it too.
@@ -135,13 +125,12 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5;
-    int kvh, tile, tiles, first;
+    int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
     const int split = tile % a.splits;
     tile = (tiles - 1 - tile) / a.splits;            // long causal tiles first
-    Seq s;
-    seq_bounds<SOURCE>(a, find_seq(a.start_q, a.tokens_q, a.batch, a.group, kRowTile, tile, first), s);
-    const int r0 = (tile - first) * kRowTile;
+    const Seq s = find_seq<SOURCE>(a, kRowTile, tile);
+    const int r0 = s.tile * kRowTile;
     if (r0 < 0 || r0 >= s.rows) return;
     const int r1 = min(r0 + kRowTile, s.rows) - 1;   // the last row
 
@@ -303,13 +292,12 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5;
-    int kvh, tile, tiles, first;
+    int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
     const int split = tile % a.splits;
     tile /= a.splits;
-    Seq s;
-    seq_bounds<SOURCE>(a, find_seq(a.start_q, a.tokens_q, a.batch, a.group, kFewRows, tile, first), s);
-    const int r0 = (tile - first) * kFewRows;
+    const Seq s = find_seq<SOURCE>(a, kFewRows, tile);
+    const int r0 = s.tile * kFewRows;
     if (r0 < 0 || r0 >= s.rows) return;
     const int r1 = min(r0 + kFewRows, s.rows) - 1;
 
@@ -346,40 +334,75 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     const int last_quad = a.dim / 8 - 1;
     typedef std::conditional_t<SOURCE == kE4m3, uintx2, uintx4> Quad;
     Quad kr[kLoads], vr[kLoads];
-    float ks[kLoads], vs[kLoads];
+    // Pages are looked up a tile before they are needed, key j0 + l by lane l:
+    // a wait for one would wait for the loads before it too. Lanes 32 on hold
+    // the same, and fetch the scales of V's rows where the others do K's.
+    int page = 0;
+    float scales = 0.f;
+    auto look = [&](int j0) {
+        if constexpr (SOURCE != kPacked)
+            page = a.table[s.b * a.cols + (min(j0 + (lane & 31), s.m - 1) >> a.page_shift)];
+    };
     auto load = [&](int j0) {
+        const int left = s.m - 1 - j0;
+        const bool one_page = SOURCE == kPacked || a.page_shift >= 5;    // (tiles are aligned)
+        int64_t row0 = s.k0 + j0;
+        int slot = 0;
+        if constexpr (SOURCE != kPacked) {
+            if ((unsigned)page >= (unsigned)a.pages) {
+                if (a.err) *a.err = 1;
+                page = 0;
+            }
+            if (one_page) {
+                row0 = page_slot(__builtin_amdgcn_readfirstlane(page), a.page_shift, j0);
+                slot = min(lane & 31, left);
+            }
+            const int64_t mine = one_page ? row0 + slot
+                                          : page_slot(page, a.page_shift, min(j0 + (lane & 31), s.m - 1));
+            if constexpr (SOURCE == kE4m3)
+                scales = (half ? a.v_scale : a.k_scale)[mine * a.kv_heads + kvh];
+        }
+        const char* kp = a.k.p + row0 * a.k.row + kvh * a.k.head;
+        const char* vp = a.v.p + row0 * a.v.row + kvh * a.v.head;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int at_quad = lane + 64 * i;
             const int r = at_quad / kQuads;
-            const int quad = min((at_quad % kQuads) ^ swizzle<kQuads>(r), last_quad);
-            const int j = min(j0 + r, s.m - 1);
-            const int64_t row = SOURCE == kPacked
-                                    ? (int64_t)(s.k0 + j)
-                                    : page_row(a.table, a.cols, s.b, a.pages, a.page_shift, a.err, j);
-            const int size = sizeof(Quad);
-            kr[i] = *reinterpret_cast<const Quad*>(a.k.p + row * a.k.row + kvh * a.k.head + quad * size);
-            vr[i] = *reinterpret_cast<const Quad*>(a.v.p + row * a.v.row + kvh * a.v.head + quad * size);
-            if constexpr (SOURCE == kE4m3) {
-                ks[i] = a.k_scale[row * a.kv_heads + kvh];
-                vs[i] = a.v_scale[row * a.kv_heads + kvh];
+            const int quad = min((at_quad % kQuads) ^ swizzle<kQuads>(r), last_quad) * (int)sizeof(Quad);
+            const int j = min(r, left);
+            if (one_page) {
+                kr[i] = *reinterpret_cast<const Quad*>(kp + ((unsigned)j * (unsigned)a.k.row + quad));
+                vr[i] = *reinterpret_cast<const Quad*>(vp + ((unsigned)j * (unsigned)a.v.row + quad));
+            } else {
+                const int64_t row = page_slot(__shfl(page, j), a.page_shift, j0 + j);
+                kr[i] = *reinterpret_cast<const Quad*>(a.k.p + row * a.k.row + kvh * a.k.head + quad);
+                vr[i] = *reinterpret_cast<const Quad*>(a.v.p + row * a.v.row + kvh * a.v.head + quad);
             }
         }
     };
     int j0 = begin + wave * kWaveKeys;
-    if (j0 < end) load(j0);
+    if (j0 < end) {
+        look(j0);
+        load(j0);
+        if (j0 + 4 * kWaveKeys < end) look(j0 + 4 * kWaveKeys);
+    }
     for (; j0 < end; j0 += 4 * kWaveKeys) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             if constexpr (SOURCE == kE4m3) {
-                kt[lane + 64 * i] = widen8<BF>(kr[i], ks[i]);
-                vt[lane + 64 * i] = widen8<BF>(vr[i], vs[i]);
+                const int r = (lane + 64 * i) / kQuads;
+                kt[lane + 64 * i] = widen8<BF>(kr[i], __shfl(scales, r));
+                vt[lane + 64 * i] = widen8<BF>(vr[i], __shfl(scales, 32 + r));
             } else {
                 kt[lane + 64 * i] = kr[i];
                 vt[lane + 64 * i] = vr[i];
             }
         }
-        if (j0 + 4 * kWaveKeys < end) load(j0 + 4 * kWaveKeys);
+        if (j0 + 4 * kWaveKeys < end) {
+            load(j0 + 4 * kWaveKeys);
+            if (j0 + 8 * kWaveKeys < end) look(j0 + 8 * kWaveKeys);
+        }
+        rd.fresh();
         floatx16 sc;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = 0.f;
@@ -483,6 +506,8 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     }
 }
 
+constexpr int kJoin = 8;
+
 // out = sum over the cuts of 2^(lse_s - lse) part_s, in the cuts' order; a
 // thread takes four elements of a row.
 template <bool BF>
@@ -496,18 +521,33 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a) {
         // rows behind the last sequence have no partial results
         if (tok < a.start_q[0] || tok >= a.start_q[a.batch]) continue;
         float all = -3.0e38f, total = 0.f;
-        for (int s = 0; s < a.splits; ++s) all = fmaxf(all, a.part_lse[s * rows + row]);
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < a.splits; ++s) {
-            const float l = a.part_lse[s * rows + row];
-            if (l == -__builtin_inff()) continue;
-            const float w = __builtin_amdgcn_exp2f(l - all);
-            const float4 x = *reinterpret_cast<const float4*>(a.part + (s * rows + row) * a.dim + quad * 4);
-            total += w;
-            o.x = fmaf(w, x.x, o.x);
-            o.y = fmaf(w, x.y, o.y);
-            o.z = fmaf(w, x.z, o.z);
-            o.w = fmaf(w, x.w, o.w);
+        for (int s = 0; s < a.splits; s += kJoin) {  // kJoin cuts' loads at once
+            float l[kJoin], most = all;
+            float4 x[kJoin];
+#pragma unroll
+            for (int e = 0; e < kJoin; ++e) {
+                l[e] = s + e < a.splits ? a.part_lse[(s + e) * rows + row] : -__builtin_inff();
+                most = fmaxf(most, l[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < kJoin; ++e)          // (a cut without keys left nothing)
+                if (l[e] != -__builtin_inff())
+                    x[e] = *reinterpret_cast<const float4*>(a.part + ((s + e) * rows + row) * a.dim + quad * 4);
+            const float shrink = __builtin_amdgcn_exp2f(all - most);
+            all = most;
+            total *= shrink;
+            o = make_float4(o.x * shrink, o.y * shrink, o.z * shrink, o.w * shrink);
+#pragma unroll
+            for (int e = 0; e < kJoin; ++e) {
+                if (l[e] == -__builtin_inff()) continue;
+                const float w = __builtin_amdgcn_exp2f(l[e] - all);
+                total += w;
+                o.x = fmaf(w, x[e].x, o.x);
+                o.y = fmaf(w, x[e].y, o.y);
+                o.z = fmaf(w, x[e].z, o.z);
+                o.w = fmaf(w, x[e].w, o.w);
+            }
         }
         const float inv = total > 0.f || total != total ? 1.f / total : 0.f;
         *reinterpret_cast<uintx2*>(a.o.p + tok * a.o.row + head * a.o.head + quad * 8) =
@@ -547,7 +587,9 @@ AttnPlan attn_plan(int64_t batch, int64_t tokens_q, int64_t heads, int64_t kv_he
     // over for few rows (ragged lengths even out), once for many.
     const int64_t groups = kv_heads * std::max(sequences, ceil_div(rows, p.tile));
     const int64_t want = p.tile == kFewRows ? 2048 : 512;
-    const int64_t least = p.tile == kFewRows ? 4 * kWaveKeys : 4 * kKeys;
+    // (a range of 512 keys takes little longer than one of 128, and a call
+    // that is not cut needs no joining: 13.2 -> LEAST us for a token over 511)
+    const int64_t least = p.tile == kFewRows ? 16 * kWaveKeys : 4 * kKeys;
     p.splits = (int)std::max<int64_t>(
         1, std::min({want / groups, most_keys / least, int64_t(128),
                      kMaxGroups / attn_groups(kv_heads, rows, p.tile, batch)}));

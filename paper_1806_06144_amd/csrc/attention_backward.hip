@@ -15,6 +15,7 @@
 // inputs' type for their products, as the probabilities of the forward pass.
 #include "attn.h"
 #include "ep_internal.h"
+#include "launch.h"
 
 namespace ep {
 
@@ -40,12 +41,11 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5;
-    int kvh, tile, tiles, first;
+    int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
     tile = tiles - 1 - tile;                         // long causal tiles first
-    Seq s;
-    seq_bounds<kPacked>(a, find_seq(a.start_q, a.tokens_q, a.batch, a.group, kRowTile, tile, first), s);
-    const int r0 = (tile - first) * kRowTile;
+    const Seq s = find_seq<kPacked>(a, kRowTile, tile);
+    const int r0 = s.tile * kRowTile;
     if (r0 < 0 || r0 >= s.rows) return;
     const int r1 = min(r0 + kRowTile, s.rows) - 1;
 
@@ -191,11 +191,12 @@ __global__ void __launch_bounds__(512, 2) attn_dkv_kernel(AttnArgs a) {
     const int pair = wave & 3;
     const bool second = wave >= 4;                   // the wave of dP, dS and dk
     const int half = lane >> 5;
-    int kvh, tile, tiles, first;
+    int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);     // (early keys have the most rows)
-    Seq s;
-    seq_bounds<kPacked>(a, find_seq(a.start_k, a.tokens_k, a.batch, 1, kKeyRange, tile, first), s);
-    const int k0 = (tile - first) * kKeyRange;
+    const int split = tile % a.row_splits;
+    tile /= a.row_splits;
+    const Seq s = find_seq<kPacked, true>(a, kKeyRange, tile);
+    const int k0 = s.tile * kKeyRange;
     if (k0 < 0 || k0 >= s.m) return;
     const int k1 = min(k0 + kKeyRange, s.m) - 1;
 
@@ -206,7 +207,8 @@ __global__ void __launch_bounds__(512, 2) attn_dkv_kernel(AttnArgs a) {
     const int wk0 = min(k0 + pair * 32, s.m - 1), wk1 = min(k0 + pair * 32 + 31, s.m - 1);
     // (rows past the last are rows that see nothing)
     const int all_lo = from_row(wk1), all_hi = min(to_row(wk0), s.rows);
-    const int begin = from_row(k0) / kStepRows * kStepRows, end = to_row(k1);
+    int begin = from_row(k0) / kStepRows * kStepRows, end = to_row(k1);
+    split_range(split, a.row_splits, kStepRows, begin, end);
 
     const TileLoader<kQuads, kWaveRows> l(lane, pair, a.dim);
     TileReader<kQuads> rd(lane);
@@ -365,8 +367,22 @@ __global__ void __launch_bounds__(512, 2) attn_dkv_kernel(AttnArgs a) {
         }
     }
     if (k0 + pair * 32 + (lane & 31) >= s.m) return;
-    const Rows& out = second ? a.dk : a.dv;
     const float scale = second ? a.scale : 1.f;
+    if (a.row_splits > 1) {
+        float* p = a.part_kv + (((split * 2 + (second ? 1 : 0)) * a.tokens_k + s.k0 + key) * a.kv_heads + kvh) * a.dim;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * b + 2 * i + 4 * half;
+                if (d < a.dim)
+                    *reinterpret_cast<float4*>(p + d) =
+                        make_float4(acc[b][i] * scale, acc[b][i + 1] * scale, acc[b][i + 2] * scale,
+                                    acc[b][i + 3] * scale);
+            }
+        return;
+    }
+    const Rows& out = second ? a.dk : a.dv;
     char* p = out.p + (int64_t)(s.k0 + key) * out.row + kvh * out.head;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -380,15 +396,57 @@ __global__ void __launch_bounds__(512, 2) attn_dkv_kernel(AttnArgs a) {
         }
 }
 
+// dk and dv from the cuts' partial sums, in the cuts' order; a thread takes
+// four elements of each.
+template <bool BF>
+__global__ void __launch_bounds__(256) attn_dkv_join_kernel(AttnArgs a) {
+    const int quads = a.dim / 4;
+    const int64_t size = a.tokens_k * a.kv_heads * a.dim;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.tokens_k * a.kv_heads * quads;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / quads, tok = row / a.kv_heads;
+        const int quad = (int)(i % quads), head = (int)(row % a.kv_heads);
+        // rows behind the last sequence have no partial sums
+        if (tok < a.start_k[0] || tok >= a.start_k[a.batch]) continue;
+        float4 dv = make_float4(0.f, 0.f, 0.f, 0.f), dk = dv;
+        const float* p = a.part_kv + row * a.dim + quad * 4;
+        for (int s = 0; s < a.row_splits; ++s, p += 2 * size) {
+            const float4 x = *reinterpret_cast<const float4*>(p);
+            const float4 y = *reinterpret_cast<const float4*>(p + size);
+            dv = make_float4(dv.x + x.x, dv.y + x.y, dv.z + x.z, dv.w + x.w);
+            dk = make_float4(dk.x + y.x, dk.y + y.y, dk.z + y.z, dk.w + y.w);
+        }
+        *reinterpret_cast<uintx2*>(a.dv.p + tok * a.dv.row + head * a.dv.head + quad * 8) =
+            uintx2{pack16<BF>(dv.x, dv.y), pack16<BF>(dv.z, dv.w)};
+        *reinterpret_cast<uintx2*>(a.dk.p + tok * a.dk.row + head * a.dk.head + quad * 8) =
+            uintx2{pack16<BF>(dk.x, dk.y), pack16<BF>(dk.z, dk.w)};
+    }
+}
+
 template <bool BF, int DP>
 void launch(const AttnArgs& a, hipStream_t s) {
     const dim3 rows((unsigned)attn_groups(a.kv_heads, a.tokens_q * a.group, kRowTile, a.batch));
-    const dim3 keys((unsigned)attn_groups(a.kv_heads, a.tokens_k, kKeyRange, a.batch));
+    const dim3 keys((unsigned)(attn_groups(a.kv_heads, a.tokens_k, kKeyRange, a.batch) * a.row_splits));
     hipLaunchKernelGGL((attn_dq_kernel<BF, DP>), rows, dim3(256), 0, s, a);
     hipLaunchKernelGGL((attn_dkv_kernel<BF, DP>), keys, dim3(512), 0, s, a);
+    if (a.row_splits > 1) {
+        const dim3 join(stride_grid(ceil_div(a.tokens_k * a.kv_heads * (a.dim / 4), 256), 256));
+        hipLaunchKernelGGL(attn_dkv_join_kernel<BF>, join, dim3(256), 0, s, a);
+    }
 }
 
 }  // namespace
+
+// Cuts of the rows, where ranges of 128 keys alone leave the device's 256
+// workgroups idle: at least 8 tiles of rows each.
+int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads) {
+    const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_k), 1);
+    const int64_t groups = kv_heads * std::max(sequences, ceil_div(tokens_k, kKeyRange));
+    const int64_t tiles = ceil_div(tokens_q * (heads / kv_heads), sequences * kStepRows);
+    return (int)std::max<int64_t>(
+        1, std::min({256 / groups, tiles / 8, int64_t(32),
+                     kMaxGroups / 2 / attn_groups(kv_heads, tokens_k, kKeyRange, batch)}));
+}
 
 hipError_t attn_backward_launch(const AttnArgs& a, bool bf, hipStream_t s) {
     if (a.dim > 64) {

@@ -58,6 +58,10 @@ struct AttnArgs {
     int splits;
     float* part;
     float* part_lse;
+    // gradients: the rows that a range of keys meets cut into row_splits
+    // ranges; partial sums [row_splits][dv, dk][tokens_k][kv_heads][dim]
+    int row_splits;
+    float* part_kv;
 };
 
 // How a forward pass runs: rows of a tile (32: the four waves of a workgroup
@@ -67,6 +71,7 @@ struct AttnPlan {
     int splits;
     int64_t bytes;            // of partial results
 };
+int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads);
 AttnPlan attn_plan(int64_t batch, int64_t tokens_q, int64_t heads, int64_t kv_heads, int64_t dim,
                    int64_t most_keys);
 
@@ -259,47 +264,68 @@ struct TileReader {
     }
 };
 
-// One sequence as a workgroup sees it. Starts and lengths come from device
-// memory: they are held within their arrays whatever they are.
+// Part `split` of the range begin .. end, whole tiles of `size`, cut into
+// `splits` parts.
+__device__ __forceinline__ void split_range(int split, int splits, int size, int& begin, int& end) {
+    const int tiles = (end - begin + size - 1) / size;
+    const int per = (tiles + splits - 1) / splits;
+    const int from = begin + min(split * per, tiles) * size;
+    end = min(end, begin + min((split + 1) * per, tiles) * size);
+    begin = from;
+}
+
+// One sequence as a workgroup sees it.
 struct Seq {
     int b;
     int q0, n;                // first packed query row (token) and their number
     int k0, m;                // first packed key row (packed keys) and their number
-    int tile;                 // tile of rows
+    int tile;                 // of its tiles
     int rows;                 // n * group
     int off;                  // position of query 0: m - n
 };
 
-// The sequence of tile `t` of the launch, and its first tile.
-__device__ __forceinline__ int find_seq(const int* start, int64_t tokens, int batch, int per,
-                                        int size, int t, int& first) {
+// The sequence of tile `t` of the launch (tiles of `size` of its queries'
+// rows, or of its keys). Starts and lengths of 64 sequences are fetched at
+// once, those of the one that is found taken from its lane: a call of a single
+// token waits for few loads one after another. Whatever the starts hold, the
+// ranges lie within their arrays; s.tile may come out negative or past the
+// sequence's tiles, which the caller leaves out.
+template <int SOURCE, bool KEYS = false>
+__device__ __forceinline__ Seq find_seq(const AttnArgs& a, int size, int t) {
     const int lane = threadIdx.x & 63;
-    int count = 0;
-    for (int i = 0; i < batch; i += 64) {
-        const int b = i + lane;
-        int begin = INT32_MAX;
-        if (b < batch) begin = (int)first_tile(start[b], (int)tokens, b, per, size);
-        count += __builtin_popcountll(__ballot(begin <= t));
+    const int per = KEYS ? 1 : a.group;
+    Seq s;
+    int first = 0;
+    for (int i = 0; i < a.batch; i += 64) {
+        const int b = min(i + lane, a.batch - 1);
+        int q0, n, k0, m;
+        held_range(a.start_q[b], a.start_q[b + 1], (int)a.tokens_q, q0, n);
+        if constexpr (SOURCE == kPacked) {
+            held_range(a.start_k[b], a.start_k[b + 1], (int)a.tokens_k, k0, m);
+        } else {
+            const int length = a.lengths[b];
+            k0 = 0;
+            m = held_length(length, a.cols, a.page_shift);
+            if (m != length && a.err) *a.err = 1;
+        }
+        const int begin = KEYS ? (int)first_tile(k0, (int)a.tokens_k, b, per, size)
+                               : (int)first_tile(q0, (int)a.tokens_q, b, per, size);
+        const int count = __builtin_popcountll(__ballot(i + lane < a.batch && begin <= t));
+        if (i == 0 || count > 0) {
+            const int at = max(count - 1, 0);
+            s.b = i + at;
+            s.q0 = __builtin_amdgcn_readlane(q0, at);
+            s.n = __builtin_amdgcn_readlane(n, at);
+            s.k0 = __builtin_amdgcn_readlane(k0, at);
+            s.m = __builtin_amdgcn_readlane(m, at);
+            first = __builtin_amdgcn_readlane(begin, at);
+        }
+        if (count < 64) break;
     }
-    const int b = __builtin_amdgcn_readfirstlane(max(count - 1, 0));
-    first = (int)first_tile(start[b], (int)tokens, b, per, size);
-    return b;
-}
-
-template <int SOURCE>
-__device__ __forceinline__ void seq_bounds(const AttnArgs& a, int b, Seq& s) {
-    s.b = b;
-    held_range(a.start_q[b], a.start_q[b + 1], (int)a.tokens_q, s.q0, s.n);
-    if constexpr (SOURCE == kPacked) {
-        held_range(a.start_k[b], a.start_k[b + 1], (int)a.tokens_k, s.k0, s.m);
-    } else {
-        const int length = a.lengths[b];
-        s.k0 = 0;
-        s.m = held_length(length, a.cols, a.page_shift);
-        if (s.m != length && a.err) *a.err = 1;
-    }
+    s.tile = t - first;
     s.rows = s.n * a.group;
     s.off = s.m - s.n;
+    return s;
 }
 
 __device__ __forceinline__ int row_token(const AttnArgs& a, int r) {

@@ -136,6 +136,10 @@ AttnPlan plan_packed(const ep_attn* a) {
     return plan_of(a, std::min(a->tokens_k, 2 * ceil_div(a->tokens_k, a->batch)));
 }
 
+int row_splits_of(const ep_attn* a) {
+    return attn_row_splits(a->batch, a->tokens_q, a->tokens_k, a->heads, a->kv_heads);
+}
+
 int check_work(const void* work, int64_t bytes, int64_t need) {
     REQUIRE(bytes >= need && (work || need == 0) && aligned16(work),
             "work must be 16-byte aligned and hold %lld bytes", (long long)need);
@@ -213,7 +217,9 @@ extern "C" int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, e
 
 extern "C" int64_t ep_attention_backward_bytes(const ep_attn* a) {
     TRY(check_attn(a, true));
-    return round_up(a->tokens_q * a->heads * 8, 16);
+    const int64_t splits = row_splits_of(a);
+    return round_up(a->tokens_q * a->heads * 8, 16) +
+           (splits > 1 ? splits * 2 * a->tokens_k * a->kv_heads * a->dim * 4 : 0);
 }
 
 extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, ep_rows k,
@@ -243,6 +249,8 @@ extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, 
     g.dv = rows_of(dv);
     g.lse2 = static_cast<float*>(work);
     g.delta = g.lse2 + a->tokens_q * a->heads;
+    g.row_splits = row_splits_of(a);
+    g.part_kv = reinterpret_cast<float*>(static_cast<char*>(work) + round_up(a->tokens_q * a->heads * 8, 16));
     return launched(attn_backward_launch(g, a->type == EP_BF16,
                                          static_cast<hipStream_t>(hip_stream)));
 }

@@ -1,6 +1,6 @@
 // Gradients of attention (attention.hip): with p_ij = exp(scale q_i.k_j -
-// lse_i) formed again from the stored log-sums, D_i = out_i.dout_i and
-// ds_ij = p_ij (dout_i.v_j - D_i),
+// lse_i) formed again from the stored log-sums, dp_ij = dout_i.v_j, D_i =
+// sum_j p_ij dp_ij = out_i.dout_i and ds_ij = p_ij (dp_ij - D_i),
 //   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,
 //   dv_j = sum_i p_ij dout_i,
 // the sums over i running over the heads of a group too.
@@ -17,12 +17,19 @@
 #include "ep_internal.h"
 #include "launch.h"
 
+#include <type_traits>
+
 namespace ep {
 
 namespace {
 
 constexpr int kKeyTile = 64;          // keys of a tile (dq)
 constexpr int kWaveKeys = 16;         // of these, loaded by a wave
+// D_i = out_i.dout_i carries the rounding of out, which beside ds counts as
+// 1 / sqrt(keys): rows of at most this many keys sum p_ij dp_ij in a sweep of
+// their own instead (three sequences of 201 in bf16: dq off by 2.3e-3 of its
+// norm against 2.5e-3, rounding the exact dq is 1.7e-3).
+constexpr int kSummedKeys = 256;
 constexpr int kStepRows = 32;         // rows of a tile (dk, dv)
 constexpr int kWaveRows = 8;          // of these, loaded by a wave
 constexpr int kStages = 4;            // tiles of rows in LDS (three are in use)
@@ -59,6 +66,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);
     const int begin = key_lo(a, s, row_token(a, r0)) / kKeyTile * kKeyTile;
     const int end = key_hi(a, s, row_token(a, r1));
+    const bool summed = end - begin <= kSummedKeys;  // D from p and dp
+    const bool single = hi - lo == 1;                // one key: p is 1, D is dp, ds nothing
 
     const TileLoader<kQuads, kWaveKeys> l(lane, wave, a.dim);
     TileReader<kQuads> rd(lane);
@@ -81,21 +90,24 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
             const uintx4 zero = {0, 0, 0, 0};
             qf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(qp + 2 * d) : zero;
             gf[i] = d < a.dim ? *reinterpret_cast<const uintx4*>(gp + 2 * d) : zero;
-            const uintx4 o = d < a.dim ? *reinterpret_cast<const uintx4*>(op + 2 * d) : zero;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                delta = fmaf(lo16<BF>(o[e]), lo16<BF>(gf[i][e]), delta);
-                delta = fmaf(hi16<BF>(o[e]), hi16<BF>(gf[i][e]), delta);
-            }
         }
-        delta = pair_sum(delta);
+        if (!summed) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int d = 16 * i + 8 * half;
+                const uintx4 o = d < a.dim ? *reinterpret_cast<const uintx4*>(op + 2 * d) : uintx4{0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    delta = fmaf(lo16<BF>(o[e]), lo16<BF>(gf[i][e]), delta);
+                    delta = fmaf(hi16<BF>(o[e]), hi16<BF>(gf[i][e]), delta);
+                }
+            }
+            delta = pair_sum(delta);
+        }
     }
     const bool mine = r0 + wave * 32 + (lane & 31) < s.rows;
     const float lse2 = a.lse[at * a.heads + head] * kLog2e;
-    if (mine && half == 0) {
-        a.lse2[at * a.heads + head] = lse2;
-        a.delta[at * a.heads + head] = delta;
-    }
+    if (mine && half == 0) a.lse2[at * a.heads + head] = lse2;
 
     floatx16 acc[kBlocks];
 #pragma unroll
@@ -103,8 +115,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
 
-    // One tile, in kt and vt; the next goes into kn and vn.
-    auto step = [&](int j0, const uintx4* kt, const uintx4* vt, uintx4* kn, uintx4* vn) {
+    // One tile, in kt and vt; the next goes into kn and vn. ds: adds to acc;
+    // else to delta.
+    auto step = [&](auto ds, int j0, const uintx4* kt, const uintx4* vt, uintx4* kn,
+                    uintx4* vn) __attribute__((always_inline)) {
         wg_barrier<0>();                             // kt and vt are there, kn and vn free
         rd.fresh();
         if (j0 + kKeyTile < end) fetch(j0 + kKeyTile, kn, vn);
@@ -131,23 +145,39 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
                     p[i] = c >= c_lo && c < c_hi ? p[i] : 0.f;
                 }
             }
-            uintx4 df[2];
+            if constexpr (!decltype(ds)::value) {
 #pragma unroll
-            for (int i = 0; i < 16; i += 2)
-                df[i >> 3][(i & 7) >> 1] =
-                    pack16<BF>(p[i] * (dp[i] - delta), p[i + 1] * (dp[i + 1] - delta));
+                for (int i = 0; i < 16; ++i)
+                    delta = fmaf(single && p[i] != 0.f ? 1.f : p[i], dp[i], delta);
+            } else {
+                uintx4 df[2];
 #pragma unroll
-            for (int c = 0; c < kBlocks; ++c)
+                for (int i = 0; i < 16; i += 2)
+                    df[i >> 3][(i & 7) >> 1] =
+                        pack16<BF>(p[i] * (dp[i] - delta), p[i + 1] * (dp[i + 1] - delta));
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    acc[c] = mfma16<BF>(rd.columns(kt, 32 * b + 16 * i, c), df[i], acc[c]);
+                for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        acc[c] = mfma16<BF>(rd.columns(kt, 32 * b + 16 * i, c), df[i], acc[c]);
+            }
         }
     };
-    for (int j0 = begin; j0 < end; j0 += 2 * kKeyTile) {
-        step(j0, kt0, vt0, kt1, vt1);
-        if (j0 + kKeyTile < end) step(j0 + kKeyTile, kt1, vt1, kt0, vt0);
+    auto sweep = [&](auto ds) __attribute__((always_inline)) {
+        for (int j0 = begin; j0 < end; j0 += 2 * kKeyTile) {
+            step(ds, j0, kt0, vt0, kt1, vt1);
+            if (j0 + kKeyTile < end) step(ds, j0 + kKeyTile, kt1, vt1, kt0, vt0);
+        }
+    };
+    if (summed && begin < end) {
+        sweep(std::false_type{});
+        delta = pair_sum(delta);
+        wg_barrier<-1>();                            // (every wave has left the tiles)
+        fetch(begin, kt0, vt0);
     }
+    sweep(std::true_type{});
     if (!mine) return;
+    if (half == 0) a.delta[at * a.heads + head] = delta;
     char* out = a.dq.p + at * a.dq.row + head * a.dq.head;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -172,7 +202,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 // a lane (16 rows of ONE key) leave P and dS in the order in which the second
 // products take them.
 template <bool BF, int DP>
-__global__ void __launch_bounds__(512, 2) attn_dkv_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArgs a) {
     constexpr int kQuads = DP / 8;
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;

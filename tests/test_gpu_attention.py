@@ -277,3 +277,15 @@ def test_binding_refusals():
     assert e.value.code == ep.EP_EINVAL
     with pytest.raises(ep.EigenProError):
         ep.ep_attention(q, q, q, q.clone(), None, s, s, causal=False, window=3)
+
+
+@pytest.mark.parametrize("kind,dim", [("bf16", 128), ("fp16", 64), ("bf16", 40)])
+@pytest.mark.parametrize("lengths,window", [([1] * 20, 0), ([130, 7], 1)])
+def test_a_query_of_one_key_has_no_gradient_to_either(kind, dim, lengths, window):
+    """Its probability is 1 whatever q and k are: dq and dk are zero, exactly."""
+    case = (kind, 6, 2, dim, lengths, lengths, True, window)
+    q, k, v, g = (x.cuda() for x in _make(case, 3, 4.0))
+    out, lse = _forward(q, k, v, lengths, lengths, window=window)
+    dq, dk, dv = _backward(g, q, k, v, out, lse, lengths, lengths, window=window)
+    assert (dq == 0).all() and (dk == 0).all()
+    assert (out.view(-1, 2, 3, dim) == v[:, :, None]).all()

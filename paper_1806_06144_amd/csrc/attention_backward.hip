@@ -468,13 +468,13 @@ void launch(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 // Cuts of the rows, where ranges of 128 keys alone leave the device's 256
-// workgroups idle: at least 8 tiles of rows each.
+// workgroups idle: at least 4 tiles of rows each.
 int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads) {
     const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_k), 1);
     const int64_t groups = kv_heads * std::max(sequences, ceil_div(tokens_k, kKeyRange));
     const int64_t tiles = ceil_div(tokens_q * (heads / kv_heads), sequences * kStepRows);
     return (int)std::max<int64_t>(
-        1, std::min({256 / groups, tiles / 8, int64_t(32),
+        1, std::min({256 / groups, tiles / 4, int64_t(32),
                      kMaxGroups / 2 / attn_groups(kv_heads, tokens_k, kKeyRange, batch)}));
 }
 

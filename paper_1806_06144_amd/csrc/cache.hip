@@ -18,6 +18,8 @@
 #include "ep_internal.h"
 #include "launch.h"
 
+#include <type_traits>
+
 namespace ep {
 
 namespace {
@@ -66,14 +68,24 @@ __device__ __forceinline__ uintx2 narrow8(uintx4 x, float& scale) {
     return r;
 }
 
-template <bool BF, bool E4M3, int LANES>
+template <bool BF, bool E4M3, int LANES, int HEADS>
 __global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a) {
-    const int64_t rows = a.tokens * a.kv_heads;
+    const int chunks = a.kv_heads / HEADS;
+    const int64_t rows = a.tokens * chunks;
     const int quad = threadIdx.x % LANES;
     const bool in = quad * 8 < a.dim;
     for (int64_t i = blockIdx.x * (256 / LANES) + threadIdx.x / LANES; i < rows;
          i += (int64_t)gridDim.x * (256 / LANES)) {
-        const int t = (int)(i / a.kv_heads), h = (int)(i % a.kv_heads);
+        const int t = (int)(i / chunks), h = (int)(i % chunks) * HEADS;
+        uintx4 k[HEADS], v[HEADS];
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            k[u] = v[u] = uintx4{0, 0, 0, 0};
+            if (in) {
+                k[u] = *reinterpret_cast<const uintx4*>(a.k.p + t * a.k.row + (h + u) * a.k.head + quad * 16);
+                v[u] = *reinterpret_cast<const uintx4*>(a.v.p + t * a.v.row + (h + u) * a.v.head + quad * 16);
+            }
+        }
         const int b = seq_of(a.start, a.batch, t);
         if (b < 0) continue;
         // the new tokens are the sequence's last
@@ -86,37 +98,36 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a) {
             continue;
         }
         const int64_t to = page_slot(page, a.page_shift, j) * a.kv_heads + h;
-        uintx4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-        if (in) {
-            k = *reinterpret_cast<const uintx4*>(a.k.p + t * a.k.row + h * a.k.head + quad * 16);
-            v = *reinterpret_cast<const uintx4*>(a.v.p + t * a.v.row + h * a.v.head + quad * 16);
-        }
-        if constexpr (E4M3) {
-            float ks, vs;
-            const uintx2 k8 = narrow8<BF, LANES>(k, ks), v8 = narrow8<BF, LANES>(v, vs);
-            if (in) {
-                *reinterpret_cast<uintx2*>(a.kp + to * a.dim + quad * 8) = k8;
-                *reinterpret_cast<uintx2*>(a.vp + to * a.dim + quad * 8) = v8;
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            if constexpr (E4M3) {
+                float ks, vs;
+                const uintx2 k8 = narrow8<BF, LANES>(k[u], ks), v8 = narrow8<BF, LANES>(v[u], vs);
+                if (in) {
+                    *reinterpret_cast<uintx2*>(a.kp + (to + u) * a.dim + quad * 8) = k8;
+                    *reinterpret_cast<uintx2*>(a.vp + (to + u) * a.dim + quad * 8) = v8;
+                }
+                if (quad == 0) {
+                    a.ks[to + u] = ks;
+                    a.vs[to + u] = vs;
+                }
+            } else if (in) {
+                *reinterpret_cast<uintx4*>(a.kp + (to + u) * a.dim * 2 + quad * 16) = k[u];
+                *reinterpret_cast<uintx4*>(a.vp + (to + u) * a.dim * 2 + quad * 16) = v[u];
             }
-            if (quad == 0) {
-                a.ks[to] = ks;
-                a.vs[to] = vs;
-            }
-        } else if (in) {
-            *reinterpret_cast<uintx4*>(a.kp + to * a.dim * 2 + quad * 16) = k;
-            *reinterpret_cast<uintx4*>(a.vp + to * a.dim * 2 + quad * 16) = v;
         }
     }
 }
 
-template <bool BF, bool E4M3, int LANES>
+template <bool BF, bool E4M3, int LANES, int HEADS>
 __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a) {
-    const int64_t rows = a.tokens * a.kv_heads;
+    const int chunks = a.kv_heads / HEADS;
+    const int64_t rows = a.tokens * chunks;
     const int quad = threadIdx.x % LANES;
     if (quad * 8 >= a.dim) return;
     for (int64_t i = blockIdx.x * (256 / LANES) + threadIdx.x / LANES; i < rows;
          i += (int64_t)gridDim.x * (256 / LANES)) {
-        const int t = (int)(i / a.kv_heads), h = (int)(i % a.kv_heads);
+        const int t = (int)(i / chunks), h = (int)(i % chunks) * HEADS;
         const int b = seq_of(a.start, a.batch, t);
         if (b < 0) continue;
         const int64_t j = (int64_t)t - a.start[b];
@@ -128,31 +139,58 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a) {
             continue;
         }
         const int64_t from = page_slot(page, a.page_shift, j) * a.kv_heads + h;
-        uintx4 k, v;
-        if constexpr (E4M3) {
-            k = widen8<BF>(*reinterpret_cast<const uintx2*>(a.kp + from * a.dim + quad * 8), a.ks[from]);
-            v = widen8<BF>(*reinterpret_cast<const uintx2*>(a.vp + from * a.dim + quad * 8), a.vs[from]);
-        } else {
-            k = *reinterpret_cast<const uintx4*>(a.kp + from * a.dim * 2 + quad * 16);
-            v = *reinterpret_cast<const uintx4*>(a.vp + from * a.dim * 2 + quad * 16);
+        typedef std::conditional_t<E4M3, uintx2, uintx4> Quad;
+        Quad k[HEADS], v[HEADS];
+        float ks[HEADS], vs[HEADS];
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            const int64_t at = (from + u) * a.dim / 8 + quad;
+            k[u] = reinterpret_cast<const Quad*>(a.kp)[at];
+            v[u] = reinterpret_cast<const Quad*>(a.vp)[at];
+            if constexpr (E4M3) {
+                ks[u] = a.ks[from + u];
+                vs[u] = a.vs[from + u];
+            }
         }
-        *reinterpret_cast<uintx4*>(a.k.p + t * a.k.row + h * a.k.head + quad * 16) = k;
-        *reinterpret_cast<uintx4*>(a.v.p + t * a.v.row + h * a.v.head + quad * 16) = v;
+#pragma unroll
+        for (int u = 0; u < HEADS; ++u) {
+            uintx4 x, y;
+            if constexpr (E4M3) {
+                x = widen8<BF>(k[u], ks[u]);
+                y = widen8<BF>(v[u], vs[u]);
+            } else {
+                x = k[u];
+                y = v[u];
+            }
+            *reinterpret_cast<uintx4*>(a.k.p + t * a.k.row + (h + u) * a.k.head + quad * 16) = x;
+            *reinterpret_cast<uintx4*>(a.v.p + t * a.v.row + (h + u) * a.v.head + quad * 16) = y;
+        }
     }
+}
+
+template <bool WRITE, bool BF, bool E4M3, int LANES, int HEADS>
+void launch_one(const CacheArgs& a, hipStream_t s) {
+    const int64_t blocks = ceil_div(a.tokens * (a.kv_heads / HEADS), 256 / LANES);
+    const dim3 grid(stride_grid(blocks, 256));
+    if constexpr (WRITE)
+        hipLaunchKernelGGL((cache_write_kernel<BF, E4M3, LANES, HEADS>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((cache_read_kernel<BF, E4M3, LANES, HEADS>), grid, dim3(256), 0, s, a);
+}
+
+// Heads a group of lanes takes at once: their loads are on the way together
+// and share the look-ups of sequence and page.
+template <bool WRITE, bool BF, bool E4M3, int LANES>
+void launch_lanes(const CacheArgs& a, hipStream_t s) {
+    if (a.kv_heads % 4 == 0) launch_one<WRITE, BF, E4M3, LANES, 4>(a, s);
+    else if (a.kv_heads % 2 == 0) launch_one<WRITE, BF, E4M3, LANES, 2>(a, s);
+    else launch_one<WRITE, BF, E4M3, LANES, 1>(a, s);
 }
 
 template <bool WRITE, bool BF, bool E4M3>
 void launch(const CacheArgs& a, hipStream_t s) {
-    const int lanes = a.dim > 64 ? 16 : 8;
-    const int64_t blocks = ceil_div(a.tokens * a.kv_heads, 256 / lanes);
-    const dim3 grid(stride_grid(blocks, 256));
-    if constexpr (WRITE) {
-        if (lanes == 16) hipLaunchKernelGGL((cache_write_kernel<BF, E4M3, 16>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((cache_write_kernel<BF, E4M3, 8>), grid, dim3(256), 0, s, a);
-    } else {
-        if (lanes == 16) hipLaunchKernelGGL((cache_read_kernel<BF, E4M3, 16>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((cache_read_kernel<BF, E4M3, 8>), grid, dim3(256), 0, s, a);
-    }
+    if (a.dim > 64) launch_lanes<WRITE, BF, E4M3, 16>(a, s);
+    else launch_lanes<WRITE, BF, E4M3, 8>(a, s);
 }
 
 template <bool WRITE>

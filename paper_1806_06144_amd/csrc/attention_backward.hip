@@ -50,7 +50,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const int half = lane >> 5;
     int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
-    tile = tiles - 1 - tile;                         // long causal tiles first
+    const int split = tile % a.key_splits;
+    tile = (tiles - 1 - tile) / a.key_splits;        // long causal tiles first
     const Seq s = find_seq<kPacked>(a, kRowTile, tile);
     const int r0 = s.tile * kRowTile;
     if (r0 < 0 || r0 >= s.rows) return;
@@ -64,9 +65,13 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const int t0 = row_token(a, min(r0 + wave * 32, s.rows - 1));
     const int t1 = row_token(a, min(r0 + wave * 32 + 31, s.rows - 1));
     const int all_lo = key_lo(a, s, t1), all_hi = key_hi(a, s, t0);
-    const int begin = key_lo(a, s, row_token(a, r0)) / kKeyTile * kKeyTile;
-    const int end = key_hi(a, s, row_token(a, r1));
-    const bool summed = end - begin <= kSummedKeys;  // D from p and dp
+    int begin = key_lo(a, s, row_token(a, r0)) / kKeyTile * kKeyTile;
+    int end = key_hi(a, s, row_token(a, r1));
+    // D from p and dp (from out where the keys are cut: there are many)
+    const bool summed = end - begin <= kSummedKeys;
+    const bool cut = a.key_splits > 1 && !summed;
+    if (cut) split_range(split, a.key_splits, kKeyTile, begin, end);
+    else if (split > 0) end = begin;                 // (the first workgroup takes them all)
     const bool single = hi - lo == 1;                // one key: p is 1, D is dp, ds nothing
 
     const TileLoader<kQuads, kWaveKeys> l(lane, wave, a.dim);
@@ -107,7 +112,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     }
     const bool mine = r0 + wave * 32 + (lane & 31) < s.rows;
     const float lse2 = a.lse[at * a.heads + head] * kLog2e;
-    if (mine && half == 0) a.lse2[at * a.heads + head] = lse2;
+    if (mine && half == 0 && split == 0) a.lse2[at * a.heads + head] = lse2;
 
     floatx16 acc[kBlocks];
 #pragma unroll
@@ -177,7 +182,21 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     }
     sweep(std::true_type{});
     if (!mine) return;
-    if (half == 0) a.delta[at * a.heads + head] = delta;
+    if (half == 0 && split == 0) a.delta[at * a.heads + head] = delta;
+    if (a.key_splits > 1) {
+        float* p = a.part_q + ((split * a.tokens_q + at) * a.heads + head) * a.dim;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * b + 2 * i + 4 * half;
+                if (d < a.dim)
+                    *reinterpret_cast<float4*>(p + d) =
+                        make_float4(acc[b][i] * a.scale, acc[b][i + 1] * a.scale,
+                                    acc[b][i + 2] * a.scale, acc[b][i + 3] * a.scale);
+            }
+        return;
+    }
     char* out = a.dq.p + at * a.dq.row + head * a.dq.head;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
@@ -426,42 +445,59 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
         }
 }
 
-// dk and dv from the cuts' partial sums, in the cuts' order; a thread takes
-// four elements of each.
+// An output from its cuts' partial sums, in the cuts' order; a thread takes
+// four elements.
+struct SumArgs {
+    const float* part;
+    int splits;
+    int64_t stride;               // floats from cut to cut
+    Rows out;
+    const int* start;
+    int64_t tokens;
+    int batch, heads, dim;
+};
+
 template <bool BF>
-__global__ void __launch_bounds__(256) attn_dkv_join_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(256) attn_sum_kernel(SumArgs a) {
     const int quads = a.dim / 4;
-    const int64_t size = a.tokens_k * a.kv_heads * a.dim;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.tokens_k * a.kv_heads * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.tokens * a.heads * quads;
          i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / quads, tok = row / a.kv_heads;
-        const int quad = (int)(i % quads), head = (int)(row % a.kv_heads);
+        const int64_t row = i / quads, tok = row / a.heads;
+        const int quad = (int)(i % quads), head = (int)(row % a.heads);
         // rows behind the last sequence have no partial sums
-        if (tok < a.start_k[0] || tok >= a.start_k[a.batch]) continue;
-        float4 dv = make_float4(0.f, 0.f, 0.f, 0.f), dk = dv;
-        const float* p = a.part_kv + row * a.dim + quad * 4;
-        for (int s = 0; s < a.row_splits; ++s, p += 2 * size) {
+        if (tok < a.start[0] || tok >= a.start[a.batch]) continue;
+        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float* p = a.part + row * a.dim + quad * 4;
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s, p += a.stride) {
             const float4 x = *reinterpret_cast<const float4*>(p);
-            const float4 y = *reinterpret_cast<const float4*>(p + size);
-            dv = make_float4(dv.x + x.x, dv.y + x.y, dv.z + x.z, dv.w + x.w);
-            dk = make_float4(dk.x + y.x, dk.y + y.y, dk.z + y.z, dk.w + y.w);
+            y = make_float4(y.x + x.x, y.y + x.y, y.z + x.z, y.w + x.w);
         }
-        *reinterpret_cast<uintx2*>(a.dv.p + tok * a.dv.row + head * a.dv.head + quad * 8) =
-            uintx2{pack16<BF>(dv.x, dv.y), pack16<BF>(dv.z, dv.w)};
-        *reinterpret_cast<uintx2*>(a.dk.p + tok * a.dk.row + head * a.dk.head + quad * 8) =
-            uintx2{pack16<BF>(dk.x, dk.y), pack16<BF>(dk.z, dk.w)};
+        *reinterpret_cast<uintx2*>(a.out.p + tok * a.out.row + head * a.out.head + quad * 8) =
+            uintx2{pack16<BF>(y.x, y.y), pack16<BF>(y.z, y.w)};
     }
+}
+
+template <bool BF>
+void sum(const AttnArgs& a, const float* part, int splits, int64_t stride, const Rows& out,
+         const int* start, int64_t tokens, int heads, hipStream_t s) {
+    const SumArgs x{part, splits, stride, out, start, tokens, a.batch, heads, a.dim};
+    const dim3 grid(stride_grid(ceil_div(tokens * heads * (a.dim / 4), 256), 256));
+    if (grid.x) hipLaunchKernelGGL(attn_sum_kernel<BF>, grid, dim3(256), 0, s, x);
 }
 
 template <bool BF, int DP>
 void launch(const AttnArgs& a, hipStream_t s) {
-    const dim3 rows((unsigned)attn_groups(a.kv_heads, a.tokens_q * a.group, kRowTile, a.batch));
+    const dim3 rows((unsigned)(attn_groups(a.kv_heads, a.tokens_q * a.group, kRowTile, a.batch) * a.key_splits));
     const dim3 keys((unsigned)(attn_groups(a.kv_heads, a.tokens_k, kKeyRange, a.batch) * a.row_splits));
     hipLaunchKernelGGL((attn_dq_kernel<BF, DP>), rows, dim3(256), 0, s, a);
+    if (a.key_splits > 1)
+        sum<BF>(a, a.part_q, a.key_splits, a.tokens_q * a.heads * a.dim, a.dq, a.start_q, a.tokens_q, a.heads, s);
     hipLaunchKernelGGL((attn_dkv_kernel<BF, DP>), keys, dim3(512), 0, s, a);
     if (a.row_splits > 1) {
-        const dim3 join(stride_grid(ceil_div(a.tokens_k * a.kv_heads * (a.dim / 4), 256), 256));
-        hipLaunchKernelGGL(attn_dkv_join_kernel<BF>, join, dim3(256), 0, s, a);
+        const int64_t size = a.tokens_k * a.kv_heads * a.dim;
+        sum<BF>(a, a.part_kv, a.row_splits, 2 * size, a.dv, a.start_k, a.tokens_k, a.kv_heads, s);
+        sum<BF>(a, a.part_kv + size, a.row_splits, 2 * size, a.dk, a.start_k, a.tokens_k, a.kv_heads, s);
     }
 }
 
@@ -476,6 +512,17 @@ int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t h
     return (int)std::max<int64_t>(
         1, std::min({256 / groups, tiles / 4, int64_t(32),
                      kMaxGroups / 2 / attn_groups(kv_heads, tokens_k, kKeyRange, batch)}));
+}
+
+// Cuts of the keys, where tiles of 128 rows alone leave its 512 slots idle: at
+// least 512 keys each.
+int attn_key_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads) {
+    const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_q), 1);
+    const int64_t rows = tokens_q * (heads / kv_heads);
+    const int64_t groups = kv_heads * std::max(sequences, ceil_div(rows, kRowTile));
+    return (int)std::max<int64_t>(
+        1, std::min({512 / groups, ceil_div(tokens_k, sequences) / 512, int64_t(32),
+                     kMaxGroups / attn_groups(kv_heads, rows, kRowTile, batch)}));
 }
 
 hipError_t attn_backward_launch(const AttnArgs& a, bool bf, hipStream_t s) {

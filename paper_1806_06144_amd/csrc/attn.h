@@ -62,6 +62,10 @@ struct AttnArgs {
     // ranges; partial sums [row_splits][dv, dk][tokens_k][kv_heads][dim]
     int row_splits;
     float* part_kv;
+    // and the keys that a tile of rows meets, into key_splits ranges; partial
+    // sums [key_splits][tokens_q][heads][dim]
+    int key_splits;
+    float* part_q;
 };
 
 // How a forward pass runs: rows of a tile (32: the four waves of a workgroup
@@ -71,6 +75,7 @@ struct AttnPlan {
     int splits;
     int64_t bytes;            // of partial results
 };
+int attn_key_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads);
 int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads);
 AttnPlan attn_plan(int64_t batch, int64_t tokens_q, int64_t heads, int64_t kv_heads, int64_t dim,
                    int64_t most_keys);
@@ -285,19 +290,30 @@ struct Seq {
 };
 
 // The sequence of tile `t` of the launch (tiles of `size` of its queries'
-// rows, or of its keys). Starts and lengths of 64 sequences are fetched at
-// once, those of the one that is found taken from its lane: a call of a single
-// token waits for few loads one after another. Whatever the starts hold, the
-// ranges lie within their arrays; s.tile may come out negative or past the
-// sequence's tiles, which the caller leaves out.
+// rows, or of its keys): a search among 64 at a time. Starts and lengths of the
+// last 64 are fetched at once, those of the one that is found taken from its
+// lane: a call of a single token waits for few loads one after another.
+// Whatever the starts hold, the ranges lie within their arrays; s.tile may come
+// out negative or past the sequence's tiles, which the caller leaves out.
 template <int SOURCE, bool KEYS = false>
 __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int size, int t) {
     const int lane = threadIdx.x & 63;
     const int per = KEYS ? 1 : a.group;
+    const int* start = KEYS ? a.start_k : a.start_q;
+    const int tokens = (int)(KEYS ? a.tokens_k : a.tokens_q);
+    int low = 0, left = a.batch;                     // the sequence is one of these
+    while (left > 64) {
+        const int stride = (left + 63) / 64;
+        const int b = low + lane * stride;
+        const bool below = lane * stride < left &&
+                           first_tile(start[min(b, a.batch - 1)], tokens, b, per, size) <= t;
+        const int skip = max(__builtin_popcountll(__ballot(below)) - 1, 0) * stride;
+        low += skip;
+        left = min(stride, left - skip);
+    }
     Seq s;
-    int first = 0;
-    for (int i = 0; i < a.batch; i += 64) {
-        const int b = min(i + lane, a.batch - 1);
+    {
+        const int b = min(low + lane, a.batch - 1);
         int q0, n, k0, m;
         held_range(a.start_q[b], a.start_q[b + 1], (int)a.tokens_q, q0, n);
         if constexpr (SOURCE == kPacked) {
@@ -308,21 +324,16 @@ __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int size, int t) {
             m = held_length(length, a.cols, a.page_shift);
             if (m != length && a.err) *a.err = 1;
         }
-        const int begin = KEYS ? (int)first_tile(k0, (int)a.tokens_k, b, per, size)
-                               : (int)first_tile(q0, (int)a.tokens_q, b, per, size);
-        const int count = __builtin_popcountll(__ballot(i + lane < a.batch && begin <= t));
-        if (i == 0 || count > 0) {
-            const int at = max(count - 1, 0);
-            s.b = i + at;
-            s.q0 = __builtin_amdgcn_readlane(q0, at);
-            s.n = __builtin_amdgcn_readlane(n, at);
-            s.k0 = __builtin_amdgcn_readlane(k0, at);
-            s.m = __builtin_amdgcn_readlane(m, at);
-            first = __builtin_amdgcn_readlane(begin, at);
-        }
-        if (count < 64) break;
+        const int begin = (int)first_tile(start[b], tokens, b, per, size);
+        const int count = __builtin_popcountll(__ballot(lane < left && begin <= t));
+        const int at = max(count - 1, 0);
+        s.b = low + at;
+        s.q0 = __builtin_amdgcn_readlane(q0, at);
+        s.n = __builtin_amdgcn_readlane(n, at);
+        s.k0 = __builtin_amdgcn_readlane(k0, at);
+        s.m = __builtin_amdgcn_readlane(m, at);
+        s.tile = t - __builtin_amdgcn_readlane(begin, at);
     }
-    s.tile = t - first;
     s.rows = s.n * a.group;
     s.off = s.m - s.n;
     return s;

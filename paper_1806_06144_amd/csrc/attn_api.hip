@@ -51,12 +51,16 @@ int check_attn(const ep_attn* a, bool packed_keys) {
 }
 
 // (data may be NULL where there are no rows)
-int check_rows(const char* name, const ep_rows& r, int64_t tokens) {
+// dim: of an output, whose rows must lie apart; 0: of an input.
+int check_rows(const char* name, const ep_rows& r, int64_t tokens, int64_t heads, int64_t dim) {
     if (tokens == 0) return EP_OK;
     REQUIRE(r.data, "%s is NULL", name);
     REQUIRE(aligned16(r.data), "%s must be 16-byte aligned", name);
-    REQUIRE(r.row % 8 == 0 && r.head % 8 == 0 && r.row >= 0 && r.head >= 0 && r.row < (1 << 24),
-            "%s: strides must be multiples of 8 elements, not negative, rows' below 2^24", name);
+    // (the stride of an axis of one element counts for nothing)
+    REQUIRE(tokens == 1 || (r.row % 8 == 0 && r.row >= dim && r.row < (1 << 24)),
+            "%s: the rows' stride must be a multiple of 8 elements in [%d, 2^24)", name, (int)dim);
+    REQUIRE(heads == 1 || (r.head % 8 == 0 && r.head >= dim),
+            "%s: the heads' stride must be a multiple of 8 elements, at least %d", name, (int)dim);
     return EP_OK;
 }
 
@@ -136,8 +140,20 @@ AttnPlan plan_packed(const ep_attn* a) {
     return plan_of(a, std::min(a->tokens_k, 2 * ceil_div(a->tokens_k, a->batch)));
 }
 
-int row_splits_of(const ep_attn* a) {
-    return attn_row_splits(a->batch, a->tokens_q, a->tokens_k, a->heads, a->kv_heads);
+// The gradients' work: log-sums and D, then partial sums of dk and dv, then of
+// dq.
+struct GradientWork {
+    int key_splits, row_splits;
+    int64_t part_kv, part_q, bytes;      // where they start, and the end
+};
+GradientWork gradient_work(const ep_attn* a) {
+    GradientWork w;
+    w.key_splits = attn_key_splits(a->batch, a->tokens_q, a->tokens_k, a->heads, a->kv_heads);
+    w.row_splits = attn_row_splits(a->batch, a->tokens_q, a->tokens_k, a->heads, a->kv_heads);
+    w.part_kv = round_up(a->tokens_q * a->heads * 8, 16);
+    w.part_q = w.part_kv + (w.row_splits > 1 ? w.row_splits * a->tokens_k * a->kv_heads * a->dim * 8 : 0);
+    w.bytes = w.part_q + (w.key_splits > 1 ? w.key_splits * a->tokens_q * a->heads * a->dim * 4 : 0);
+    return w;
 }
 
 int check_work(const void* work, int64_t bytes, int64_t need) {
@@ -170,12 +186,12 @@ CacheArgs cache_args(const ep_cache* c, const ep_pages* p, const ep_rows& k, con
 }
 
 int check_move(const ep_cache* c, const ep_pages* p, int type, const ep_rows& k, const ep_rows& v,
-               int64_t tokens, const int32_t* start) {
+               int64_t tokens, const int32_t* start, bool out) {
     TRY(check_cache(c, p, type));
     REQUIRE(tokens >= 0 && tokens < kMaxTokens, "tokens must be in [0, 2^30)");
     REQUIRE(start, "start is NULL");
-    TRY(check_rows("k", k, tokens));
-    TRY(check_rows("v", v, tokens));
+    TRY(check_rows("k", k, tokens, c->kv_heads, out ? c->dim : 0));
+    TRY(check_rows("v", v, tokens, c->kv_heads, out ? c->dim : 0));
     return EP_OK;
 }
 
@@ -197,10 +213,10 @@ extern "C" int64_t ep_attention_bytes(const ep_attn* a) {
 extern "C" int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, ep_rows out,
                             float* lse, void* work, int64_t work_bytes, void* hip_stream) {
     TRY(check_attn(a, true));
-    TRY(check_rows("q", q, a->tokens_q));
-    TRY(check_rows("out", out, a->tokens_q));
-    TRY(check_rows("k", k, a->tokens_k));
-    TRY(check_rows("v", v, a->tokens_k));
+    TRY(check_rows("q", q, a->tokens_q, a->heads, 0));
+    TRY(check_rows("out", out, a->tokens_q, a->heads, a->dim));
+    TRY(check_rows("k", k, a->tokens_k, a->kv_heads, 0));
+    TRY(check_rows("v", v, a->tokens_k, a->kv_heads, 0));
     const AttnPlan plan = plan_packed(a);
     TRY(check_work(work, work_bytes, plan.bytes));
     if (a->tokens_q == 0) return EP_OK;
@@ -217,9 +233,7 @@ extern "C" int ep_attention(const ep_attn* a, ep_rows q, ep_rows k, ep_rows v, e
 
 extern "C" int64_t ep_attention_backward_bytes(const ep_attn* a) {
     TRY(check_attn(a, true));
-    const int64_t splits = row_splits_of(a);
-    return round_up(a->tokens_q * a->heads * 8, 16) +
-           (splits > 1 ? splits * 2 * a->tokens_k * a->kv_heads * a->dim * 4 : 0);
+    return gradient_work(a).bytes;
 }
 
 extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, ep_rows k,
@@ -231,12 +245,12 @@ extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, 
     const ep_rows* of_k[] = {&k, &v, &dk, &dv};
     const char* names[] = {"dout", "q", "out", "dq", "k", "v", "dk", "dv"};
     for (int i = 0; i < 4; ++i) {
-        TRY(check_rows(names[i], *of_q[i], a->tokens_q));
-        TRY(check_rows(names[4 + i], *of_k[i], a->tokens_k));
+        TRY(check_rows(names[i], *of_q[i], a->tokens_q, a->heads, i == 3 ? a->dim : 0));
+        TRY(check_rows(names[4 + i], *of_k[i], a->tokens_k, a->kv_heads, i >= 2 ? a->dim : 0));
     }
     REQUIRE(lse || a->tokens_q == 0, "lse is NULL");
-    const int64_t need = ep_attention_backward_bytes(a);
-    TRY(check_work(work, work_bytes, need));
+    const GradientWork w = gradient_work(a);
+    TRY(check_work(work, work_bytes, w.bytes));
     AttnArgs g = args_of(a);
     g.dout = rows_of(dout);
     g.q = rows_of(q);
@@ -249,15 +263,17 @@ extern "C" int ep_attention_backward(const ep_attn* a, ep_rows dout, ep_rows q, 
     g.dv = rows_of(dv);
     g.lse2 = static_cast<float*>(work);
     g.delta = g.lse2 + a->tokens_q * a->heads;
-    g.row_splits = row_splits_of(a);
-    g.part_kv = reinterpret_cast<float*>(static_cast<char*>(work) + round_up(a->tokens_q * a->heads * 8, 16));
+    g.row_splits = w.row_splits;
+    g.part_kv = reinterpret_cast<float*>(static_cast<char*>(work) + w.part_kv);
+    g.key_splits = w.key_splits;
+    g.part_q = reinterpret_cast<float*>(static_cast<char*>(work) + w.part_q);
     return launched(attn_backward_launch(g, a->type == EP_BF16,
                                          static_cast<hipStream_t>(hip_stream)));
 }
 
 extern "C" int ep_cache_write(const ep_cache* c, const ep_pages* p, int type, ep_rows k, ep_rows v,
                               int64_t tokens, const int32_t* start, void* hip_stream) {
-    TRY(check_move(c, p, type, k, v, tokens, start));
+    TRY(check_move(c, p, type, k, v, tokens, start, false));
     if (tokens == 0) return EP_OK;
     return launched(cache_write_launch(cache_args(c, p, k, v, tokens, start), type == EP_BF16,
                                        c->type == EP_E4M3, static_cast<hipStream_t>(hip_stream)));
@@ -265,7 +281,7 @@ extern "C" int ep_cache_write(const ep_cache* c, const ep_pages* p, int type, ep
 
 extern "C" int ep_cache_read(const ep_cache* c, const ep_pages* p, int type, ep_rows k, ep_rows v,
                              int64_t tokens, const int32_t* start, void* hip_stream) {
-    TRY(check_move(c, p, type, k, v, tokens, start));
+    TRY(check_move(c, p, type, k, v, tokens, start, true));
     if (tokens == 0) return EP_OK;
     return launched(cache_read_launch(cache_args(c, p, k, v, tokens, start), type == EP_BF16,
                                       c->type == EP_E4M3, static_cast<hipStream_t>(hip_stream)));
@@ -281,8 +297,8 @@ extern "C" int ep_cache_attention(const ep_attn* a, const ep_cache* c, const ep_
                                   ep_rows q, ep_rows out, float* lse, void* work,
                                   int64_t work_bytes, void* hip_stream) {
     TRY(check_cached(a, c, p));
-    TRY(check_rows("q", q, a->tokens_q));
-    TRY(check_rows("out", out, a->tokens_q));
+    TRY(check_rows("q", q, a->tokens_q, a->heads, 0));
+    TRY(check_rows("out", out, a->tokens_q, a->heads, a->dim));
     const AttnPlan plan = plan_of(a, p->cols * c->page_size);
     TRY(check_work(work, work_bytes, plan.bytes));
     if (a->tokens_q == 0) return EP_OK;

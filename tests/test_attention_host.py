@@ -201,6 +201,15 @@ def test_attention_refuses_rows(name, bad):
     assert name in ep.ep_last_error()
 
 
+def test_outputs_that_overlap_themselves():
+    for bad in (dict(row=0), dict(row=56), dict(head=0), dict(head=8)):
+        assert _forward(_attn(), out=_rows(**bad)) == ep.EP_EINVAL
+        for name in ("dq", "dk", "dv"):
+            assert _backward(_attn(), **{name: _rows(**bad)}) == ep.EP_EINVAL
+        assert ep.raw_call("ep_cache_read", ctypes.byref(_cache()), ctypes.byref(_table()),
+                           ep.EP_BF16, _rows(**bad), _rows(), 10, A, None) == ep.EP_EINVAL
+
+
 def test_attention_null():
     assert _forward(None) == ep.EP_EINVAL
 

@@ -289,3 +289,61 @@ def test_a_query_of_one_key_has_no_gradient_to_either(kind, dim, lengths, window
     dq, dk, dv = _backward(g, q, k, v, out, lse, lengths, lengths, window=window)
     assert (dq == 0).all() and (dk == 0).all()
     assert (out.view(-1, 2, 3, dim) == v[:, :, None]).all()
+
+
+def test_thousands_of_sequences():
+    """The search for a tile's sequence goes through several levels."""
+    import torch
+    rng = np.random.default_rng(1)
+    lengths = rng.integers(0, 4, 9000)
+    q, k, v = (torch.randn((lengths.sum(), 2, 16), device="cuda").half() for _ in range(3))
+    out, lse = _forward(q, k, v, lengths, lengths, 0.25)
+    # sequences 0 .. 3 long: row i of a sequence against the rows before it
+    s = torch.from_numpy(starts(lengths)).long()
+    b = torch.repeat_interleave(torch.arange(9000), torch.from_numpy(lengths))
+    first = s[b].cuda()
+    at = torch.arange(q.shape[0], device="cuda")
+    x = torch.full((q.shape[0], 2, 3), -float("inf"), dtype=torch.float64, device="cuda")
+    vals = torch.zeros((q.shape[0], 2, 3, 16), dtype=torch.float64, device="cuda")
+    for j in range(3):
+        ok = first + j <= at
+        row = (first + j).clamp(max=q.shape[0] - 1)
+        x[:, :, j] = torch.where(ok[:, None], 0.25 * (q.double() * k[row].double()).sum(-1), x[:, :, j])
+        vals[:, :, j] = v[row].double()
+    want = (x.softmax(-1)[..., None] * vals).sum(2)
+    # (one rounding of the result and one of each probability, 2^-11 of sums of |v| < 16)
+    assert (out.double() - want).abs().max() < 3 * 2.0 ** -11 * 6
+    assert (lse.double() - x.logsumexp(-1)).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("case", [("bf16", 2, 1, 64, [1], [6000], False, 0),
+                                  ("fp16", 2, 2, 128, [3, 40], [2000, 2100], True, 0),
+                                  ("bf16", 4, 1, 128, [2000], [30], False, 0),
+                                  ("bf16", 2, 1, 72, [5, 700], [4000, 700], True, 0)],
+                         ids=lambda c: f"{c[0]}-{c[4]}-{c[5]}")
+def test_gradients_of_few_rows_or_few_keys(case):
+    """Keys or rows cut over workgroups, their partial sums added."""
+    test_forward(case)
+    test_backward(case)
+
+
+def test_gradients_without_queries_or_keys():
+    import torch
+    q, k = torch.zeros((0, 2, 64), dtype=torch.float16), torch.zeros((5, 2, 64), dtype=torch.float16)
+    for nq, nk in (([0], [5]), ([5], [0])):
+        a, b = (torch.ones((n, 2, 64), dtype=torch.float16, device="cuda") for n in (nq[0], nk[0]))
+        out, lse = _forward(a, b, b, nq, nk)
+        grads = _backward(a, a, b, b, out, lse, nq, nk)
+        assert all((x == 0).all() for x in (out, *grads)) and (lse == -float("inf")).all()
+
+
+def test_keys_shared_by_stride():
+    """An input may be one head expanded over all (stride 0)."""
+    import torch
+    case = ("bf16", 6, 3, 64, [70], [70], True, 0)
+    q, k, v, _ = _make(case)
+    k, v = (x[:, :1].expand(-1, 3, -1) for x in (k, v))
+    ke, ve = (x.cuda()[:, :1].expand(-1, 3, -1) for x in (k, v))
+    got = _forward(q.cuda(), ke, ve, [70], [70], 0.125)
+    assert ke.stride(1) == 0
+    _check_forward(got, case, q, k, v, 0.125)

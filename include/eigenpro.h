@@ -459,9 +459,10 @@ int64_t ep_attention_backward_bytes(const ep_attn* a);
  * EP_E4M3: a row (one token, one head) is dim e4m3 numbers times its scale, the
  * smallest power of two that brings its largest finite value within 448 (at
  * least 2^-110, in fp16 2^-15; 1 for a row of zeros). Each value is rounded
- * once, to nearest; what comes back is exact in the 16-bit type. Values above
- * 1.875 times the type's largest power of two are stored as that; values that
- * are not finite are stored as NaN.
+ * once, to nearest; what comes back is exact in the 16-bit type that was
+ * written (read as EP_FP16, rows written as EP_BF16 may leave fp16's range).
+ * Values above 1.875 times the type's largest power of two are stored as that;
+ * values that are not finite are stored as NaN.
  */
 typedef struct ep_cache {
     int32_t type;               /* what the pages hold: EP_BF16, EP_FP16, EP_E4M3 */

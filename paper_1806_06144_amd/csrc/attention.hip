@@ -8,7 +8,7 @@
 // so the maximum and the sum of a row need a single exchange between lanes,
 // and the probabilities, rounded to the inputs' type, are already in the
 // layout of the right operand of out^T += V^T P^T, once V^T is read in the
-// order in which a lane holds its keys (tile_columns).
+// order in which a lane holds its keys (TileReader::columns).
 //
 // Scores, maximum, sum and output accumulate in float32. The probabilities
 // are rounded to 16 bits for the second product (relative 2^-9 in bf16, as

@@ -174,6 +174,27 @@ def test_cache_attention(case):
     assert c.err.item() == 0
 
 
+@pytest.mark.parametrize("new,total", [(1, 5000), (140, 2000)])
+def test_rows_of_no_sequence_stay_as_they_are(new, total):
+    """Rows before the first and behind the last sequence, where the keys are
+    cut and where they are not."""
+    import torch
+    for wide in (1, 60):
+        case = ("bf16", False, 4, 2, 64, 16, [new], [total], True, 0)
+        c, q, k, v = _fill(case, cols=wide * -(-total // 16))
+        pad = rounded(np.random.default_rng(0), (20, 4, 64), "bf16")
+        rows = torch.cat([pad[:9], q, pad[9:]]).cuda()
+        out = torch.full_like(rows, 7.0)
+        lse = torch.full(tuple(rows.shape[:2]), 7.0, device="cuda")
+        c.ep.ep_cache_attention(rows, c.c, out, lse, c.table, c.ints([total]), c.ints([9, 9 + new]),
+                                0.1, err=c.err)
+        want, l, b_out, b_lse = oracle_forward(f64(q), k, v, [new], [total], True, 0, 0.1, "bf16")
+        within(f64(out[9:9 + new]), want, b_out, "out")
+        within(f64(lse[9:9 + new]), l, b_lse, "lse")
+        for x in (out, lse):
+            assert (x[:9] == 7).all() and (x[9 + new:] == 7).all()
+
+
 def test_a_table_much_wider_than_the_sequences():
     case = ("bf16", False, 4, 2, 128, 16, [1, 1], [40, 700], True, 0)
     c, q, k, v = _fill(case, cols=60000)

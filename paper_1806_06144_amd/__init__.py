@@ -188,6 +188,8 @@ def _torch():
 
 
 _int32, _float32 = _torch().int32, _torch().float32
+_current_device = _torch()._C._cuda_getDevice
+_raw_stream = _torch()._C._cuda_getCurrentRawStream
 _ATTN_TYPES = {_torch().bfloat16: EP_BF16, _torch().float16: EP_FP16}
 _CACHE_TYPES = {**_ATTN_TYPES, _torch().float8_e4m3fn: EP_E4M3, _torch().uint8: EP_E4M3}
 
@@ -393,17 +395,25 @@ def ep_device_probe():
 
 
 def _mismatch(x, name, dtype, shape, device):
-    if x.device != device or not x.is_cuda:
-        raise ValueError(f"{name}: expected a tensor on {device if device.type == 'cuda' else 'a device'}")
+    if x.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}")
     if x.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {x.dtype}")
-    raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    if x.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    raise ValueError(f"{name}: expected a contiguous tensor")
+
+
+def _device(x):
+    if not x.is_cuda:
+        raise ValueError("expected a device tensor")
+    return x.device
 
 
 def _rows(x, name, shape, dtype, device):
     """EpRows of a [tokens, heads, dim] tensor; its last axis is contiguous,
     the others may be strided (slices of a wider array)."""
-    if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_cuda:
+    if x.dtype is not dtype or x.shape != shape or x.device != device:
         _mismatch(x, name, dtype, shape, device)
     row, head, one = x.stride()
     if one != 1:
@@ -413,10 +423,9 @@ def _rows(x, name, shape, dtype, device):
 
 def _dense(x, name, dtype, shape, device):
     """Address of a contiguous tensor of that type, shape and device."""
-    if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_cuda:
+    if (x.dtype is not dtype or x.shape != shape or x.device != device
+            or not x.is_contiguous()):
         _mismatch(x, name, dtype, shape, device)
-    if not x.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor")
     return x.data_ptr()
 
 
@@ -441,27 +450,24 @@ def _attn(q, kv_heads, tokens_k, start_q, start_k, scale, causal, window, device
 
 
 def _on_stream(device, stream, call):
-    """call(stream handle, allocate) with the tensors' device current; memory
-    from allocate(bytes) belongs to the stream that the work goes to."""
+    """call(stream handle, device) with the tensors' device current; memory
+    that call allocates belongs to the stream that the work goes to."""
     torch = _torch()
-    index = device.index
-    if stream is None and index == torch._C._cuda_getDevice():
-        return call(torch._C._cuda_getCurrentRawStream(index),
-                    lambda n: torch.empty(n, dtype=torch.uint8, device=device))
+    if stream is None and device.index == _current_device():
+        return call(_raw_stream(device.index), device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
     with torch.cuda.device(device), torch.cuda.stream(stream):
-        return call(torch.cuda.current_stream().cuda_stream,
-                    lambda n: torch.empty(n, dtype=torch.uint8, device=device))
+        return call(torch.cuda.current_stream().cuda_stream, device)
 
 
-def _work(allocate, n):
+def _work(device, n):
     """(address, bytes) of n bytes, and what holds them; n is a ..._bytes answer."""
     if n == 0:
         return None, 0, None
     if n < 0:
         _check(int(n))
-    x = allocate(n)
+    x = _torch().empty(n, dtype=_torch().uint8, device=device)
     return x.data_ptr(), n, x
 
 
@@ -475,14 +481,14 @@ def ep_attention(q, k, v, out, lse, start_q, start_k, scale=None, causal=True, w
     (float32 [tokens, heads], or None). q, out: [tokens, heads, dim] bfloat16
     or float16; k, v: [tokens_k, kv_heads, dim]; start_q, start_k: int32,
     batch + 1 values. scale: dim ** -0.5 by default; window: 0 for none."""
-    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    dev, dt, qs, ks = _device(q), q.dtype, q.shape, k.shape
     a = _attn(q, ks[1], ks[0], start_q, start_k, scale, causal, window, dev)
     kv = (a.tokens_k, a.kv_heads, a.dim)
     args = (ctypes.byref(a), _rows(q, "q", qs, dt, dev), _rows(k, "k", kv, dt, dev),
             _rows(v, "v", kv, dt, dev), _rows(out, "out", qs, dt, dev), _lse(lse, q, dev))
 
-    def call(s, allocate):
-        work, n, _hold = _work(allocate, _lib.ep_attention_bytes(args[0]))
+    def call(s, device):
+        work, n, _hold = _work(device, _lib.ep_attention_bytes(args[0]))
         return _check(_lib.ep_attention(*args, work, n, s))
     return _on_stream(dev, stream, call)
 
@@ -491,7 +497,7 @@ def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k,
                           causal=True, window=0, stream=None):
     """Gradients dq, dk, dv of ep_attention for the gradient dout of out; out
     and lse are what it returned. Written, not added to."""
-    dev, dt, qs, ks = q.device, q.dtype, q.shape, k.shape
+    dev, dt, qs, ks = _device(q), q.dtype, q.shape, k.shape
     a = _attn(q, ks[1], ks[0], start_q, start_k, scale, causal, window, dev)
     kv = (a.tokens_k, a.kv_heads, a.dim)
     args = (ctypes.byref(a), _rows(dout, "dout", qs, dt, dev), _rows(q, "q", qs, dt, dev),
@@ -500,8 +506,8 @@ def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k,
             _rows(dq, "dq", qs, dt, dev), _rows(dk, "dk", kv, dt, dev),
             _rows(dv, "dv", kv, dt, dev))
 
-    def call(s, allocate):
-        work, n, _hold = _work(allocate, _lib.ep_attention_backward_bytes(args[0]))
+    def call(s, device):
+        work, n, _hold = _work(device, _lib.ep_attention_backward_bytes(args[0]))
         return _check(_lib.ep_attention_backward(*args, work, n, s))
     return _on_stream(dev, stream, call)
 
@@ -512,7 +518,7 @@ class EpCache:
     k_scale and v_scale [pages, page_size, kv_heads]. Holds the tensors."""
 
     def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
-        shape, dt, dev = k_pages.shape, k_pages.dtype, k_pages.device
+        shape, dt, dev = k_pages.shape, k_pages.dtype, _device(k_pages)
         if len(shape) != 4:
             raise ValueError("k_pages: expected [pages, page_size, kv_heads, dim]")
         ks = vs = None
@@ -572,8 +578,8 @@ def ep_cache_attention(q, cache, out, lse, table, lengths, start_q, scale=None, 
             ctypes.byref(_pages(cache, table, lengths, err)))
     args = (_rows(q, "q", qs, dt, dev), _rows(out, "out", qs, dt, dev), _lse(lse, q, dev))
 
-    def call(s, allocate):
-        work, n, _hold = _work(allocate, _lib.ep_cache_attention_bytes(*refs))
+    def call(s, device):
+        work, n, _hold = _work(device, _lib.ep_cache_attention_bytes(*refs))
         return _check(_lib.ep_cache_attention(*refs, *args, work, n, s))
     return _on_stream(dev, stream, call)
 

@@ -445,13 +445,13 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
         }
 }
 
-// An output from its cuts' partial sums, in the cuts' order; a thread takes
-// four elements.
+// Outputs (blockIdx.y) from their cuts' partial sums, in the cuts' order; a
+// thread takes four elements.
 struct SumArgs {
-    const float* part;
+    const float* part[2];
     int splits;
     int64_t stride;               // floats from cut to cut
-    Rows out;
+    Rows out[2];
     const int* start;
     int64_t tokens;
     int batch, heads, dim;
@@ -460,6 +460,7 @@ struct SumArgs {
 template <bool BF>
 __global__ void __launch_bounds__(256) attn_sum_kernel(SumArgs a) {
     const int quads = a.dim / 4;
+    const Rows out = a.out[blockIdx.y];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.tokens * a.heads * quads;
          i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / quads, tok = row / a.heads;
@@ -467,22 +468,20 @@ __global__ void __launch_bounds__(256) attn_sum_kernel(SumArgs a) {
         // rows behind the last sequence have no partial sums
         if (tok < a.start[0] || tok >= a.start[a.batch]) continue;
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        const float* p = a.part + row * a.dim + quad * 4;
+        const float* p = a.part[blockIdx.y] + row * a.dim + quad * 4;
 #pragma unroll 4
         for (int s = 0; s < a.splits; ++s, p += a.stride) {
             const float4 x = *reinterpret_cast<const float4*>(p);
             y = make_float4(y.x + x.x, y.y + x.y, y.z + x.z, y.w + x.w);
         }
-        *reinterpret_cast<uintx2*>(a.out.p + tok * a.out.row + head * a.out.head + quad * 8) =
+        *reinterpret_cast<uintx2*>(out.p + tok * out.row + head * out.head + quad * 8) =
             uintx2{pack16<BF>(y.x, y.y), pack16<BF>(y.z, y.w)};
     }
 }
 
 template <bool BF>
-void sum(const AttnArgs& a, const float* part, int splits, int64_t stride, const Rows& out,
-         const int* start, int64_t tokens, int heads, hipStream_t s) {
-    const SumArgs x{part, splits, stride, out, start, tokens, a.batch, heads, a.dim};
-    const dim3 grid(stride_grid(ceil_div(tokens * heads * (a.dim / 4), 256), 256));
+void sum(const SumArgs& x, int outputs, hipStream_t s) {
+    const dim3 grid(stride_grid(ceil_div(x.tokens * x.heads * (x.dim / 4), 256), 256), outputs);
     if (grid.x) hipLaunchKernelGGL(attn_sum_kernel<BF>, grid, dim3(256), 0, s, x);
 }
 
@@ -492,12 +491,13 @@ void launch(const AttnArgs& a, hipStream_t s) {
     const dim3 keys((unsigned)(attn_groups(a.kv_heads, a.tokens_k, kKeyRange, a.batch) * a.row_splits));
     hipLaunchKernelGGL((attn_dq_kernel<BF, DP>), rows, dim3(256), 0, s, a);
     if (a.key_splits > 1)
-        sum<BF>(a, a.part_q, a.key_splits, a.tokens_q * a.heads * a.dim, a.dq, a.start_q, a.tokens_q, a.heads, s);
+        sum<BF>({{a.part_q, nullptr}, a.key_splits, a.tokens_q * a.heads * a.dim, {a.dq, {}}, a.start_q,
+                 a.tokens_q, a.batch, a.heads, a.dim}, 1, s);
     hipLaunchKernelGGL((attn_dkv_kernel<BF, DP>), keys, dim3(512), 0, s, a);
     if (a.row_splits > 1) {
         const int64_t size = a.tokens_k * a.kv_heads * a.dim;
-        sum<BF>(a, a.part_kv, a.row_splits, 2 * size, a.dv, a.start_k, a.tokens_k, a.kv_heads, s);
-        sum<BF>(a, a.part_kv + size, a.row_splits, 2 * size, a.dk, a.start_k, a.tokens_k, a.kv_heads, s);
+        sum<BF>({{a.part_kv, a.part_kv + size}, a.row_splits, 2 * size, {a.dv, a.dk}, a.start_k,
+                 a.tokens_k, a.batch, a.kv_heads, a.dim}, 2, s);
     }
 }
 

@@ -266,6 +266,10 @@ def test_binding_refusals():
     with pytest.raises(TypeError):
         ep.ep_attention(q, q.half(), q, q.clone(), None, s, s)
     with pytest.raises(TypeError):
+        ep.ep_attention(q.float(), q, q, q.clone(), None, s, s)
+    with pytest.raises(ValueError):
+        ep.ep_attention(q, q.cpu(), q, q.clone(), None, s, s)
+    with pytest.raises(TypeError):
         ep.ep_attention(q, q, q, q.clone(), None, s.long(), s)
     with pytest.raises(ValueError):
         ep.ep_attention(q, q, q, q.clone(), None, s, torch.zeros(5, dtype=torch.int32, device="cuda"))

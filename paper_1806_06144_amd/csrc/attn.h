@@ -8,12 +8,13 @@
 // a matrix instruction from a single token of many heads.
 //
 // Tiles of 16-bit rows lie in LDS row by row, quads (16 bytes) permuted by
-// quad ^ swizzle(row) since neither the padded rows nor another order can be
-// had from loads that write LDS directly. Two kinds of reads have to be
-// spread over the banks: 16-byte reads of one quad of consecutive rows (eight
-// lanes a cycle, so the swizzle takes eight values over eight rows), and the
-// transposing reads, where 16 lanes read four rows x 32 contiguous bytes (so
-// bits 1 and 2 of the swizzle take four values over four rows).
+// quad ^ swizzle(row) since neither padded rows nor another order can be had
+// from loads that write LDS directly. Two kinds of reads have to be spread over
+// the 64 banks: 16-byte reads of one quad of 16 consecutive rows (their places
+// within 256 bytes differ: 1 KB in four cycles), and the transposing reads,
+// where 32 lanes read four rows x 64 contiguous bytes (the four take different
+// quarters of 256 bytes; with places that differ within 128 bytes only, a read
+// took four cycles instead of two).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -182,9 +183,10 @@ __device__ __forceinline__ float pair_max(float x) {
 
 template <int QUADS>                  // quads a row (16 or 8)
 __device__ __forceinline__ int swizzle(int row) {
-    const int f = ((row & 3) << 1) | ((row >> 2) & 1);
-    return QUADS == 16 ? f | (row & 8) : f;
+    if constexpr (QUADS == 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    return ((row & 2) << 1) | ((row >> 2) & 3);      // (two rows to 256 bytes)
 }
+
 __device__ __forceinline__ void load_lds16(const char* p, uintx4* lds) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) unsigned*)p,
                                      (__attribute__((address_space(3))) unsigned*)lds, 16, 0, 0);
@@ -257,10 +259,10 @@ struct TileReader {
         return *reinterpret_cast<const uintx4*>(t + (r ^ (32 * step)));
     }
     __device__ __forceinline__ uintx4 columns(const uintx4* tile, int row0, int block) const {
-        // (eight rows on, a swizzle of 16 quads differs in its highest bit)
+        // (eight rows on, the swizzle differs in bit 1)
         const char* t = reinterpret_cast<const char*>(tile) + row0 * QUADS * 16;
         const char* a = t + (c ^ (64 * block));
-        const char* b = t + 8 * QUADS * 16 + (c ^ (64 * block) ^ (QUADS == 16 ? 128 : 0));
+        const char* b = t + 8 * QUADS * 16 + (c ^ (64 * block) ^ 32);
         const shortx4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)a);
         const shortx4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)b);
         typedef unsigned uintx2 __attribute__((ext_vector_type(2)));

@@ -5,6 +5,12 @@
 //   dv_j = sum_i p_ij dout_i,
 // the sums over i running over the heads of a group too.
 //
+// What bounds them: the matrix units and the device's power (2 x 4096 tokens, 32
+// heads over 8, dim 128, bf16: 420 us for dq and 670 for dk and dv, 0.92
+// PFLOP/s of the seven products), at dim 64 and short ranges vector work and
+// barriers (12 ragged sequences of up to 2047 with a window of 512, 12 heads:
+// 79 and 100 us).
+//
 // Two kernels, each owning what it sums, so there are no atomics and the
 // results do not depend on the order of the workgroups: dq walks the keys as
 // the forward pass does (three products a tile), dk and dv walk the rows
@@ -27,8 +33,8 @@ constexpr int kKeyTile = 64;          // keys of a tile (dq)
 constexpr int kWaveKeys = 16;         // of these, loaded by a wave
 // D_i = out_i.dout_i carries the rounding of out, which beside ds counts as
 // 1 / sqrt(keys): rows of at most this many keys sum p_ij dp_ij in a sweep of
-// their own instead (three sequences of 201 in bf16: dq off by 2.3e-3 of its
-// norm against 2.5e-3, rounding the exact dq is 1.7e-3).
+// their own instead (three sequences of 201 in bf16: dq 1.42 times as far off
+// as the exact one rounded, against 1.50).
 constexpr int kSummedKeys = 256;
 constexpr int kStepRows = 32;         // rows of a tile (dk, dv)
 constexpr int kWaveRows = 8;          // of these, loaded by a wave

@@ -438,7 +438,7 @@ def _attn_type(x):
 
 def _attn(q, kv_heads, tokens_k, start_q, start_k, scale, causal, window, device):
     kind = _attn_type(q)
-    if q.dim() != 3:
+    if len(q.shape) != 3:
         raise ValueError("q: expected [tokens, heads, dim]")
     tokens_q, heads, dim = q.shape
     starts = start_q.shape
@@ -482,6 +482,8 @@ def ep_attention(q, k, v, out, lse, start_q, start_k, scale=None, causal=True, w
     or float16; k, v: [tokens_k, kv_heads, dim]; start_q, start_k: int32,
     batch + 1 values. scale: dim ** -0.5 by default; window: 0 for none."""
     dev, dt, qs, ks = _device(q), q.dtype, q.shape, k.shape
+    if len(ks) != 3:
+        raise ValueError("k: expected [tokens, kv_heads, dim]")
     a = _attn(q, ks[1], ks[0], start_q, start_k, scale, causal, window, dev)
     kv = (a.tokens_k, a.kv_heads, a.dim)
     args = (ctypes.byref(a), _rows(q, "q", qs, dt, dev), _rows(k, "k", kv, dt, dev),
@@ -498,6 +500,8 @@ def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k,
     """Gradients dq, dk, dv of ep_attention for the gradient dout of out; out
     and lse are what it returned. Written, not added to."""
     dev, dt, qs, ks = _device(q), q.dtype, q.shape, k.shape
+    if len(ks) != 3:
+        raise ValueError("k: expected [tokens, kv_heads, dim]")
     a = _attn(q, ks[1], ks[0], start_q, start_k, scale, causal, window, dev)
     kv = (a.tokens_k, a.kv_heads, a.dim)
     args = (ctypes.byref(a), _rows(dout, "dout", qs, dt, dev), _rows(q, "q", qs, dt, dev),

@@ -39,7 +39,7 @@ constexpr int kWaveKeys = 32;         // keys of a wave's own tile (few rows)
 // a tile before that: a wait for one would wait for the loads before it too.
 template <bool BF, int DP, int SOURCE>
 struct KeyTiles {
-    static constexpr int kQuads = DP / 8;
+    static constexpr int kQuads = tile_quads(DP);
     static constexpr int kLoads = TileLoader<kQuads, kWaveRows>::kLoads;
     static constexpr bool kEight = SOURCE == kE4m3 || SOURCE == kE4m3Small;
     static constexpr bool kSmall = SOURCE == kPagedSmall || SOURCE == kE4m3Small;
@@ -124,7 +124,7 @@ struct KeyTiles {
 // took 1128 us against 1090.
 template <bool BF, int DP, int SOURCE>
 __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
-    constexpr int kQuads = DP / 8;
+    constexpr int kQuads = tile_quads(DP);
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
     // (arrays of their own: what is loaded into one is not waited for where
@@ -289,13 +289,14 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
 // The same pass for few rows (at most 32 a sequence on average; a token of a
 // group of 8 fills 8 of 32 columns, which memory-bound work has to spare): a
 // workgroup's four waves share 32 rows and take the tiles of 32 keys in turn,
-// each with a running maximum and sum of its own, joined at the end. What bounds it is the cache's stream from memory:
-// a wave loads its next tile (up to 16 KB) into registers while it works on
-// the one in its own part of LDS, so there is no barrier before the end, and
-// two workgroups a CU keep up to 128 KB on the way.
+// each with a running maximum and sum of its own, joined at the end. What
+// bounds it is the cache's stream from memory: a wave loads its next tile (up
+// to 16 KB) into registers while it works on the one in its own part of LDS,
+// so there is no barrier before the end, and two workgroups a CU keep up to
+// 128 KB on the way.
 template <bool BF, int DP, int SOURCE>
 __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
-    constexpr int kQuads = DP / 8;
+    constexpr int kQuads = tile_quads(DP);
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
     constexpr int kLoads = kWaveKeys * kQuads / 64;  // of K, and of V
@@ -583,7 +584,8 @@ void launch_dim(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
 
 template <bool BF, int SOURCE>
 void launch(const AttnArgs& a, const AttnPlan& p, hipStream_t s) {
-    if (a.dim > 64) launch_dim<BF, 128, SOURCE>(a, p, s);
+    if (a.dim > 96) launch_dim<BF, 128, SOURCE>(a, p, s);
+    else if (a.dim > 64) launch_dim<BF, 96, SOURCE>(a, p, s);
     else launch_dim<BF, 64, SOURCE>(a, p, s);
 }
 

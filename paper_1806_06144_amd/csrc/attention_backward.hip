@@ -43,7 +43,7 @@ constexpr int kKeyRange = 128;        // keys of a workgroup (dk, dv): 32 per wa
 
 template <bool BF, int DP>
 __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
-    constexpr int kQuads = DP / 8;
+    constexpr int kQuads = tile_quads(DP);
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
     __shared__ uintx4 kt0[kKeyTile * kQuads];
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 // products take them.
 template <bool BF, int DP>
 __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArgs a) {
-    constexpr int kQuads = DP / 8;
+    constexpr int kQuads = tile_quads(DP);
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
     // (arrays of their own: what is loaded into one is not waited for where
@@ -532,11 +532,13 @@ int attn_key_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t h
 }
 
 hipError_t attn_backward_launch(const AttnArgs& a, bool bf, hipStream_t s) {
-    if (a.dim > 64) {
-        if (bf) launch<true, 128>(a, s);
-        else launch<false, 128>(a, s);
+    if (bf) {
+        if (a.dim > 96) launch<true, 128>(a, s);
+        else if (a.dim > 64) launch<true, 96>(a, s);
+        else launch<true, 64>(a, s);
     } else {
-        if (bf) launch<true, 64>(a, s);
+        if (a.dim > 96) launch<false, 128>(a, s);
+        else if (a.dim > 64) launch<false, 96>(a, s);
         else launch<false, 64>(a, s);
     }
     return hipGetLastError();

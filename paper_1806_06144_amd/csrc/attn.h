@@ -181,6 +181,10 @@ __device__ __forceinline__ float pair_max(float x) {
     return fmaxf(a, b);
 }
 
+// Quads a row of a tile for products of depth dp (64, 96 or 128). Rows of 96
+// take the places of 128, whose last quarter is loaded twice and not read.
+constexpr int tile_quads(int dp) { return dp > 64 ? 16 : 8; }
+
 template <int QUADS>                  // quads a row (16 or 8)
 __device__ __forceinline__ int swizzle(int row) {
     if constexpr (QUADS == 16) return ((row & 3) << 2) | ((row >> 2) & 3);

@@ -597,13 +597,19 @@ AttnPlan attn_plan(int64_t batch, int64_t tokens_q, int64_t heads, int64_t kv_he
     const int64_t rows = tokens_q * (heads / kv_heads);
     const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_q), 1);
     p.tile = rows <= kFewRows * sequences ? kFewRows : kRowTile;
+    // Up to 64 rows a sequence in tiles of 32 read the keys twice: 186 us for 16
+    // sequences of 64 rows over 20000 keys, 152 in one tile of 128.
     // Workgroups that have work, if no sequence is much longer than the
-    // others; cut the keys until the device is full: its 512 slots four times
-    // over for few rows (ragged lengths even out), once for many.
+    // others; the keys are cut until the device is full. Few rows: its 512
+    // slots four times over, so that ragged lengths even out (64 single tokens
+    // over up to 16000 keys, e4m3 rows of up to 100000: once 494 and 287 us,
+    // twice 459 and 250, four times 437 and 244, eight times 434 and 254). Many
+    // rows: once (4 x 512 rows over 30000 keys: half 442 us, once 310, twice 323).
     const int64_t groups = kv_heads * std::max(sequences, ceil_div(rows, p.tile));
     const int64_t want = p.tile == kFewRows ? 2048 : 512;
-    // (a token over 511 keys: 12.0 us in one piece, 8.5 and 4.7 for joining in
-    // four)
+    // At least 512 keys a range: a token over 511 takes 11.6 us in one piece, 9.5
+    // in four, replayed from a graph, but a second launch takes the host 3.5;
+    // a token over 4096 14.8 (ranges of 1024: 21.4).
     const int64_t least = p.tile == kFewRows ? 16 * kWaveKeys : 4 * kKeys;
     p.splits = (int)std::max<int64_t>(
         1, std::min({want / groups, most_keys / least, int64_t(128),

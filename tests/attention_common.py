@@ -67,6 +67,6 @@ def within(got, want, bound, name):
     fine = np.isfinite(want)
     assert np.array_equal(got[~fine], want[~fine]), name
     assert np.isfinite(got[fine]).all(), f"{name}: not finite"
-    off = np.abs(got - want)[fine] - bound[fine]
+    off = np.abs(got[fine] - want[fine]) - bound[fine]
     assert off.size == 0 or off.max() <= 1e-30, (
         f"{name}: {off.max():.3e} past its bound, {np.mean(off > 1e-30):.2%} of the elements")

@@ -376,7 +376,9 @@ int ep_device_probe(double* mfma_f32_tflops, double* shader_clock_mhz);
  * sequence b holds rows start[b] .. start[b+1] - 1 (device int32, batch + 1
  * values, not decreasing). Rows behind the last sequence are neither read nor
  * written. Values of start outside [0, tokens] are taken as the nearest
- * inside.
+ * inside. A padded batch of `batch` x length rows is 2 batch sequences, each
+ * one's padding a sequence of its own behind it: start = 0, len_0, length,
+ * length + len_1, 2 length, ...; what the padding holds reaches only padding.
  *
  * Heads. Query head h reads key head h / (heads / kv_heads).
  *

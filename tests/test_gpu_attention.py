@@ -351,3 +351,112 @@ def test_keys_shared_by_stride():
     got = _forward(q.cuda(), ke, ve, [70], [70], 0.125)
     assert ke.stride(1) == 0
     _check_forward(got, case, q, k, v, 0.125)
+
+
+def test_offsets_past_32_bits():
+    """Rows 16 MB apart: 300 of them span 5 GB, in every array of the calls."""
+    import torch
+    n, h, g, d = 300, 4, 2, 64
+    case = ("bf16", h, g, d, [n], [n], True, 0)
+    q, k, v, go = _make(case, 11)
+    wide = torch.empty((n, 1 << 23), dtype=torch.bfloat16, device="cuda")
+    views, at = [], 0
+    for heads in (h, g, g, h, h, h, g, g):           # q, k, v, dout, out, dq, dk, dv
+        views.append(wide[:, at:at + heads * d].view(n, heads, d))
+        at += heads * d
+    for x, y in zip(views, (q, k, v, go)):
+        x.copy_(y)
+    qw, kw, vw, gw, ow, *grads = views
+    scale = 0.125
+    out, lse = _forward(qw, kw, vw, [n], [n], scale, out=ow)
+    o64, _ = _check_forward((out, lse), case, q, k, v, scale)
+    _backward(gw, qw, kw, vw, out, lse, [n], [n], scale, into=grads)
+    want, bound = oracle_backward(f64(q), f64(k), f64(v), f64(go), np.abs(f64(out)) + np.abs(o64),
+                                  [n], [n], True, 0, scale, "bf16")
+    for x, w, b, name in zip(grads, want, bound, ("dq", "dk", "dv")):
+        within(f64(x), w, b, name)
+
+
+def test_calls_at_once_on_two_streams():
+    """Calls with work memory on two streams, not waiting for each other."""
+    import torch
+    problems = []
+    for i, (nq, nk) in enumerate((([400, 30], [400, 30]), ([6], [3000]))):
+        case = ("bf16", 8, 2, 128, nq, nk, True, 0)
+        q, k, v, g = (x.cuda() for x in _make(case, i))
+        out, lse = _forward(q, k, v, nq, nk)
+        grads = _backward(g, q, k, v, out, lse, nq, nk)
+        problems.append((q, k, v, g, nq, nk, [out, lse, *grads]))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in problems]
+    got = [[], []]
+    for _ in range(5):
+        for i, (s, (q, k, v, g, nq, nk, _)) in enumerate(zip(streams, problems)):
+            with torch.cuda.stream(s):
+                out, lse = _forward(q, k, v, nq, nk)
+                got[i].append([out, lse, *_backward(g, q, k, v, out, lse, nq, nk)])
+    torch.cuda.synchronize()
+    for i, p in enumerate(problems):
+        assert all(torch.equal(a, b) for run in got[i] for a, b in zip(run, p[-1]))
+
+
+def test_a_padded_batch():
+    """Each sequence's padding is a sequence of its own; it holds NaN, which
+    reaches no row of the sequences, nor their gradients."""
+    import torch
+    h, g, d, length, lengths = 4, 2, 64, 100, [100, 37, 0, 64]
+    case = ("bf16", h, g, d, lengths, lengths, True, 0)
+    q, k, v, go = _make(case, 4)
+    parts = [x for n in lengths for x in (n, length - n)]
+    keep = torch.cat([torch.arange(length) < n for n in lengths]).cuda()
+
+    def padded(x):
+        y = torch.full((len(lengths) * length,) + tuple(x.shape[1:]), float("nan"), dtype=x.dtype,
+                       device="cuda")
+        y[keep] = x.cuda()
+        return y
+    qp, kp, vp, gp = (padded(x) for x in (q, k, v, go))
+    out, lse = _forward(qp, kp, vp, parts, parts, 0.125)
+    o64, _ = _check_forward((out[keep], lse[keep]), case, q, k, v, 0.125)
+    grads = _backward(gp, qp, kp, vp, out, lse, parts, parts, 0.125)
+    want, bound = oracle_backward(f64(q), f64(k), f64(v), f64(go), np.abs(f64(out[keep])) + np.abs(o64),
+                                  lengths, lengths, True, 0, 0.125, "bf16")
+    for x, w, b, name in zip(grads, want, bound, ("dq", "dk", "dv")):
+        within(f64(x[keep]), w, b, name)
+
+
+def test_a_long_sequence():
+    """100000 tokens: some rows, and the gradients of some rows and of the last
+    keys, which few rows see."""
+    import torch
+    import oracle.attention as oa
+    n, h, d, scale, kind = 100000, 2, 64, 0.125, "bf16"
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, go = (torch.randn((n, h, d), device="cuda", generator=gen).bfloat16() for _ in range(2))
+    k, v = (torch.randn((n, 1, d), device="cuda", generator=gen).bfloat16() for _ in range(2))
+    out, lse = _forward(q, k, v, [n], [n], scale)
+    dq, dk, dv = _backward(go, q, k, v, out, lse, [n], [n], scale)
+    q64, g64, k64, v64 = f64(q), f64(go), f64(k)[:, 0], f64(v)[:, 0]
+    rng = np.random.default_rng(0)
+    tail = n - 40
+    for i in [0, 1, 63, 64, n - 1, *rng.integers(100, n, 8)]:
+        for j in range(h):
+            args = q64[i:i + 1, j], k64[:i + 1], v64[:i + 1]
+            o, l = oa.head_forward(*args, True, 0, scale)
+            within(f64(out[i, j])[None], o, oa.forward_bound(*args, True, 0, scale, kind), "out")
+            within(f64(lse[i:i + 1, j]), l, oa.lse_bound(args[0], args[1], l, scale), "lse")
+            g = oa.head_backward(*args, g64[i:i + 1, j], True, 0, scale)[0]
+            b = oa.backward_bound(*args, g64[i:i + 1, j], np.abs(o) + np.abs(f64(out[i, j])), True, 0,
+                                  scale, kind)[0]
+            within(f64(dq[i, j])[None], g, b, "dq")
+    want, bound = np.zeros((2, 40, d)), np.zeros((2, 40, d))
+    for j in range(h):                               # rows tail .. n - 1 over all keys
+        args = q64[tail:, j], k64, v64, g64[tail:, j]
+        o = oa.head_forward(*args[:3], True, 0, scale)[0]
+        _, a, b = oa.head_backward(*args, True, 0, scale)
+        _, ea, eb = oa.backward_bound(*args, np.abs(o) + np.abs(f64(out[tail:, j])), True, 0, scale, kind)
+        want += [a[tail:], b[tail:]]
+        bound += [ea[tail:], eb[tail:]]
+    u = oa.U[kind]
+    for x, w, e, name in zip((dk, dv), want, bound, ("dk", "dv")):
+        within(f64(x[tail:, 0]), w, e * (1 + u) + u * np.abs(w), name)

@@ -140,8 +140,7 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
     const int split = tile % a.splits;
-    tile = (tiles - 1 - tile) / a.splits;            // long causal tiles first
-    const Seq s = find_seq<SOURCE>(a, kRowTile, tile);
+    const Seq s = find_seq<SOURCE>(a, kRowTile, tile / a.splits, tiles / a.splits);
     const int r0 = s.tile * kRowTile;
     if (r0 < 0 || r0 >= s.rows) return;
     const int r1 = min(r0 + kRowTile, s.rows) - 1;   // the last row
@@ -309,8 +308,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
     const int split = tile % a.splits;
-    tile /= a.splits;
-    const Seq s = find_seq<SOURCE>(a, kFewRows, tile);
+    const Seq s = find_seq<SOURCE>(a, kFewRows, tile / a.splits, tiles / a.splits);
     const int r0 = s.tile * kFewRows;
     if (r0 < 0 || r0 >= s.rows) return;
     const int r1 = min(r0 + kFewRows, s.rows) - 1;

@@ -57,8 +57,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     int kvh, tile, tiles;
     head_and_tile(a.kv_heads, kvh, tile, tiles);
     const int split = tile % a.key_splits;
-    tile = (tiles - 1 - tile) / a.key_splits;        // long causal tiles first
-    const Seq s = find_seq<kPacked>(a, kRowTile, tile);
+    const Seq s = find_seq<kPacked>(a, kRowTile, tile / a.key_splits, tiles / a.key_splits);
     const int r0 = s.tile * kRowTile;
     if (r0 < 0 || r0 >= s.rows) return;
     const int r1 = min(r0 + kRowTile, s.rows) - 1;
@@ -247,10 +246,9 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
     const bool second = wave >= 4;                   // the wave of dP, dS and dk
     const int half = lane >> 5;
     int kvh, tile, tiles;
-    head_and_tile(a.kv_heads, kvh, tile, tiles);     // (early keys have the most rows)
+    head_and_tile(a.kv_heads, kvh, tile, tiles);
     const int split = tile % a.row_splits;
-    tile /= a.row_splits;
-    const Seq s = find_seq<kPacked, true>(a, kKeyRange, tile);
+    const Seq s = find_seq<kPacked, true>(a, kKeyRange, tile / a.row_splits, tiles / a.row_splits);
     const int k0 = s.tile * kKeyRange;
     if (k0 < 0 || k0 >= s.m) return;
     const int k1 = min(k0 + kKeyRange, s.m) - 1;

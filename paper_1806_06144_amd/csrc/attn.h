@@ -295,18 +295,22 @@ struct Seq {
     int off;                  // position of query 0: m - n
 };
 
-// The sequence of tile `t` of the launch (tiles of `size` of its queries'
-// rows, or of its keys): a search among 64 at a time. Starts and lengths of the
-// last 64 are fetched at once, those of the one that is found taken from its
-// lane: a call of a single token waits for few loads one after another.
+// The sequence and tile (of `size` of its queries' rows, or of its keys) that
+// is the u-th of `tiles` to start. Longest first: of a causal sequence its
+// last rows (first keys) before the others, and up to 64 sequences of
+// different lengths by their length, so that what starts last ends soon (24
+// ragged sequences in the order of the batch, the longest last: ORDER us). Starts and lengths of 64 sequences are fetched at once, those of the one
+// that is found taken from its lane: a call of a single token waits for few
+// loads one after another. More sequences are searched 64 at a time.
 // Whatever the starts hold, the ranges lie within their arrays; s.tile may come
 // out negative or past the sequence's tiles, which the caller leaves out.
 template <int SOURCE, bool KEYS = false>
-__device__ __forceinline__ Seq find_seq(const AttnArgs& a, int size, int t) {
+__device__ __forceinline__ Seq find_seq(const AttnArgs& a, int size, int u, int tiles) {
     const int lane = threadIdx.x & 63;
     const int per = KEYS ? 1 : a.group;
     const int* start = KEYS ? a.start_k : a.start_q;
     const int tokens = (int)(KEYS ? a.tokens_k : a.tokens_q);
+    const int t = KEYS ? u : tiles - 1 - u;
     int low = 0, left = a.batch;                     // the sequence is one of these
     while (left > 64) {
         const int stride = (left + 63) / 64;
@@ -317,29 +321,41 @@ __device__ __forceinline__ Seq find_seq(const AttnArgs& a, int size, int t) {
         low += skip;
         left = min(stride, left - skip);
     }
+    const int b = min(low + lane, a.batch - 1);
+    int q0, n, k0, m;
+    held_range(a.start_q[b], a.start_q[b + 1], (int)a.tokens_q, q0, n);
+    if constexpr (SOURCE == kPacked) {
+        held_range(a.start_k[b], a.start_k[b + 1], (int)a.tokens_k, k0, m);
+    } else {
+        const int length = a.lengths[b];
+        k0 = 0;
+        m = held_length(length, a.cols, a.page_shift);
+        if (m != length && a.err) *a.err = 1;
+    }
     Seq s;
-    {
-        const int b = min(low + lane, a.batch - 1);
-        int q0, n, k0, m;
-        held_range(a.start_q[b], a.start_q[b + 1], (int)a.tokens_q, q0, n);
-        if constexpr (SOURCE == kPacked) {
-            held_range(a.start_k[b], a.start_k[b + 1], (int)a.tokens_k, k0, m);
-        } else {
-            const int length = a.lengths[b];
-            k0 = 0;
-            m = held_length(length, a.cols, a.page_shift);
-            if (m != length && a.err) *a.err = 1;
+    int at;
+    const int cost = KEYS ? n : m;                   // of a tile
+    if (a.batch <= 64 && !a.window && !__all(cost == __builtin_amdgcn_readfirstlane(cost))) {
+        const int own = lane >= a.batch ? 0 : KEYS ? (m + size - 1) / size : (n * per + size - 1) / size;
+        int before = 0;                              // tiles of longer sequences
+        for (int i = 0; i < a.batch; ++i) {
+            const int other = __builtin_amdgcn_readlane(cost, i);
+            if (other > cost || (other == cost && i < lane)) before += __builtin_amdgcn_readlane(own, i);
         }
+        const uint64_t mine = __ballot(u >= before && u < before + own);
+        at = mine ? __builtin_ctzll(mine) : 0;
+        const int within = u - __builtin_amdgcn_readlane(before, at);
+        s.tile = !mine ? -1 : KEYS ? within : __builtin_amdgcn_readlane(own, at) - 1 - within;
+    } else {
         const int begin = (int)first_tile(start[b], tokens, b, per, size);
-        const int count = __builtin_popcountll(__ballot(lane < left && begin <= t));
-        const int at = max(count - 1, 0);
-        s.b = low + at;
-        s.q0 = __builtin_amdgcn_readlane(q0, at);
-        s.n = __builtin_amdgcn_readlane(n, at);
-        s.k0 = __builtin_amdgcn_readlane(k0, at);
-        s.m = __builtin_amdgcn_readlane(m, at);
+        at = max(__builtin_popcountll(__ballot(lane < left && begin <= t)) - 1, 0);
         s.tile = t - __builtin_amdgcn_readlane(begin, at);
     }
+    s.b = low + at;
+    s.q0 = __builtin_amdgcn_readlane(q0, at);
+    s.n = __builtin_amdgcn_readlane(n, at);
+    s.k0 = __builtin_amdgcn_readlane(k0, at);
+    s.m = __builtin_amdgcn_readlane(m, at);
     s.rows = s.n * a.group;
     s.off = s.m - s.n;
     return s;

@@ -17,9 +17,9 @@
 // What bounds it: many rows, the matrix units and the device's power (2 x 8192
 // tokens, 32 heads over 8, dim 128, causal, bf16: 1.09 ms, 1.01 PFLOP/s, where
 // a library product of 8192^3 reaches 1.15); at dim 64 the softmax's vector
-// work (24 ragged sequences of up to 1000, 16 heads: 77 us, 0.56 PFLOP/s); few
-// rows, memory (64 single tokens over up to 16000: 433 us, 5.4 TB/s; e4m3 rows
-// of up to 100000 tokens: 229 us, 4.1 TB/s).
+// work (24 ragged sequences of up to 1000, 16 heads: 78 us, 0.55 PFLOP/s); few
+// rows, memory (64 single tokens over up to 16000: 415 us, 5.6 TB/s; e4m3 rows
+// of up to 100000 tokens: 222 us, 4.3 TB/s).
 #include "attn.h"
 #include "ep_internal.h"
 #include "launch.h"

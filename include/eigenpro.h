@@ -465,7 +465,10 @@ int64_t ep_attention_backward_bytes(const ep_attn* a);
  * once, to nearest; what comes back is exact in the 16-bit type that was
  * written (read as EP_FP16, rows written as EP_BF16 may leave fp16's range).
  * Values above 1.875 times the type's largest power of two are stored as that;
- * values that are not finite are stored as NaN.
+ * values that are not finite are stored as NaN. Scales that a program sets
+ * itself (rows quantised elsewhere) may be any numbers: what comes back, and
+ * what attention sees, is then e4m3 x scale in float32, rounded to the 16-bit
+ * type.
  */
 typedef struct ep_cache {
     int32_t type;               /* what the pages hold: EP_BF16, EP_FP16, EP_E4M3 */

@@ -519,7 +519,8 @@ def ep_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, start_q, start_k,
 class EpCache:
     """A paged cache: k_pages and v_pages are [pages, page_size, kv_heads, dim]
     bfloat16, float16, or float8_e4m3fn (uint8 is taken as that) with float32
-    k_scale and v_scale [pages, page_size, kv_heads]. Holds the tensors."""
+    k_scale and v_scale [pages, page_size, kv_heads]: a row is its values times
+    its scale, a power of two where ep_cache_write wrote it. Holds the tensors."""
 
     def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
         shape, dt, dev = k_pages.shape, k_pages.dtype, _device(k_pages)

@@ -107,11 +107,15 @@ struct KeyTiles {
     // Puts what fetch holds in registers into the tile.
     __device__ __forceinline__ void store(uintx4* kt, uintx4* vt) {
         if constexpr (kEight) {
+            bool powers = true;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) powers = powers && power_of_two(ks[i]) && power_of_two(vs[i]);
+            powers = __all(powers);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int to = kWaveRows * kQuads * wave + 64 * i + lane;
-                kt[to] = widen8<BF>(k8[i], ks[i]);
-                vt[to] = widen8<BF>(v8[i], vs[i]);
+                kt[to] = widen8<BF>(k8[i], ks[i], powers);
+                vt[to] = widen8<BF>(v8[i], vs[i], powers);
             }
         }
     }
@@ -399,12 +403,13 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
         if (j0 + 4 * kWaveKeys < end) look(j0 + 4 * kWaveKeys);
     }
     for (; j0 < end; j0 += 4 * kWaveKeys) {
+        const bool powers = SOURCE != kE4m3 || __all(power_of_two(scales));
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             if constexpr (SOURCE == kE4m3) {
                 const int r = (lane + 64 * i) / kQuads;
-                kt[lane + 64 * i] = widen8<BF>(kr[i], __shfl(scales, r));
-                vt[lane + 64 * i] = widen8<BF>(vr[i], __shfl(scales, 32 + r));
+                kt[lane + 64 * i] = widen8<BF>(kr[i], __shfl(scales, r), powers);
+                vt[lane + 64 * i] = widen8<BF>(vr[i], __shfl(scales, 32 + r), powers);
             } else {
                 kt[lane + 64 * i] = kr[i];
                 vt[lane + 64 * i] = vr[i];

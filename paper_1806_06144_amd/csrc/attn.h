@@ -385,10 +385,29 @@ __device__ __forceinline__ int64_t page_row(const int* table, int64_t cols, int 
 
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 
-// Eight e4m3 values times a power of two as eight 16-bit values (exact).
+// Whether the scaled conversion takes this scale: it reads the exponent alone.
+__device__ __forceinline__ bool power_of_two(float scale) {
+    return __builtin_amdgcn_frexp_mantf(scale) == 0.5f && scale >= 0x1p-126f;
+}
+
+// Eight e4m3 values times a scale as eight 16-bit values. powers: the scale is
+// a power of two in every lane (as this library writes them), so the products
+// are exact and one instruction a pair; others are formed in float32 and
+// rounded to nearest. (Looking at the scales costs 1 %: 8 x 4 tokens over 100000
+// cached ones 222.4 us without, 224.9 with.)
 template <bool BF>
-__device__ __forceinline__ uintx4 widen8(uintx2 u, float scale) {
+__device__ __forceinline__ uintx4 widen8(uintx2 u, float scale, bool powers) {
     uintx4 r;
+    if (!powers) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(u[i], false);
+            const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(u[i], true);
+            r[2 * i] = pack16<BF>(lo[0] * scale, lo[1] * scale);
+            r[2 * i + 1] = pack16<BF>(hi[0] * scale, hi[1] * scale);
+        }
+        return r;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         if constexpr (BF) {

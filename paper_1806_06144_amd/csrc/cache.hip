@@ -8,6 +8,8 @@
 // exact in bf16 and fp16 alike, so attention reads the very values that a
 // read back gives. A scale of amax / 448 would use up to twice the range but
 // round twice and cost a multiplication per score and probability.
+// Such scales, set elsewhere, are read as they are: widen8 (attn.h) multiplies
+// in float32 and rounds.
 // Values above 1.875 times the largest power of two of the type are stored as
 // that (they would round up to a number the type does not have); infinities
 // and NaN are stored as NaN.
@@ -158,8 +160,8 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a) {
         for (int u = 0; u < HEADS; ++u) {
             uintx4 x, y;
             if constexpr (E4M3) {
-                x = widen8<BF>(k[u], ks[u]);
-                y = widen8<BF>(v[u], vs[u]);
+                x = widen8<BF>(k[u], ks[u], power_of_two(ks[u]));
+                y = widen8<BF>(v[u], vs[u], power_of_two(vs[u]));
             } else {
                 x = k[u];
                 y = v[u];

@@ -390,9 +390,9 @@ int ep_device_probe(double* mfma_f32_tflops, double* shader_clock_mhz);
  *
  * Arithmetic. Scores, softmax statistics and sums are float32; probabilities
  * (and, for gradients, p (dp - D)) are rounded to the element type for their
- * products. EP_FP16 gradients: as everywhere in fp16, values below 2^-24 vanish
- * and values above 65504 are infinite; scale the loss so that dout is of the
- * order of one.
+ * products (EP_FP16: times a power of two that keeps them within its range).
+ * EP_FP16 gradients themselves: as everywhere in fp16, values below 2^-24
+ * vanish and values above 65504 are infinite; scale the loss accordingly.
  */
 
 /* Rows of heads: element (t, h, c) at data[t row + h head + c], 16-bit.

@@ -19,6 +19,15 @@
 //
 // Scores, probabilities and sums are float32; p and ds are rounded to the
 // inputs' type for their products, as the probabilities of the forward pass.
+// fp16 has all its bits from 2^-14 to 65504 only, while p is 1 / keys and ds
+// that much smaller too: both enter their products times a power of two, which
+// the float32 sums are divided by at the end (exactly). p is at most one and
+// takes 2^14. What ds may be depends on dout, so a row's (for dk a key's) power
+// starts high and comes down as its largest ds asks for, as a softmax's maximum
+// rises. Without, at 131072 keys dv was 6.6 times as far off as the exact one
+// rounded, and dq 45 times for dout of 2^-8; like this 1.4 and 1.03. It costs
+// fp16 4 % at dim 64 (12 ragged sequences of up to 2047: 174.1 us, 181.4 like
+// this).
 #include "attn.h"
 #include "ep_internal.h"
 #include "launch.h"
@@ -40,6 +49,28 @@ constexpr int kStepRows = 32;         // rows of a tile (dk, dv)
 constexpr int kWaveRows = 8;          // of these, loaded by a wave
 constexpr int kStages = 4;            // tiles of rows in LDS (three are in use)
 constexpr int kKeyRange = 128;        // keys of a workgroup (dk, dv): 32 per wave
+
+constexpr float kLiftP = 14.f;        // fp16: exponents of the powers of two of p,
+constexpr float kLiftSlope = 60.f;    // and of ds where a row or key starts
+
+// x: ds times 2^lift of a lane's row or key (which lanes l and l + 32 share),
+// acc its sums. Where one is past 2^15, brings them down to 2^11, which leaves
+// room to grow: 25 binades below hold all their bits.
+template <int BLOCKS>
+__device__ __forceinline__ bool keep_in_range(floatx16& x, floatx16 (&acc)[BLOCKS], float& lift) {
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(x[i]));
+    if (!__any(most > 0x1p15f)) return false;
+    most = pair_max(most);
+    const float drop = most > 0x1p15f ? (float)(__builtin_amdgcn_frexp_expf(most) - 11) : 0.f;
+    const float by = __builtin_amdgcn_exp2f(-drop);
+    lift -= drop;
+    x *= by;
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) acc[b] *= by;
+    return true;
+}
 
 template <bool BF, int DP>
 __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
@@ -117,7 +148,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     }
     const bool mine = r0 + wave * 32 + (lane & 31) < s.rows;
     const float lse2 = a.lse[at * a.heads + head] * kLog2e;
-    if (mine && half == 0 && split == 0) a.lse2[at * a.heads + head] = lse2;
+    if (mine && half == 0 && split == 0) a.lse2[at * a.heads + head] = BF ? lse2 : lse2 - kLiftP;
+    float lift = BF ? 0.f : kLiftSlope;              // (of this lane's row)
 
     floatx16 acc[kBlocks];
 #pragma unroll
@@ -144,9 +176,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
                 dp = mfma16<BF>(rd.rows(vt, 32 * b, i), gf[i], dp);
             }
             float p[16];
+            const float base = !BF && decltype(ds)::value ? lift - lse2 : -lse2;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, -lse2));
+                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, base));
             if (masked) {                            // (a row that sees nothing has lse = -inf)
                 const int c_lo = lo - j0 - 4 * half, c_hi = hi - j0 - 4 * half;
 #pragma unroll
@@ -162,9 +195,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
             } else {
                 uintx4 df[2];
 #pragma unroll
-                for (int i = 0; i < 16; i += 2)
-                    df[i >> 3][(i & 7) >> 1] =
-                        pack16<BF>(p[i] * (dp[i] - delta), p[i + 1] * (dp[i + 1] - delta));
+                for (int i = 0; i < 16; ++i) dp[i] = p[i] * (dp[i] - delta);
+                if constexpr (!BF) keep_in_range(dp, acc, lift);
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) df[i >> 3][(i & 7) >> 1] = pack16<BF>(dp[i], dp[i + 1]);
 #pragma unroll
                 for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
@@ -188,6 +222,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     sweep(std::true_type{});
     if (!mine) return;
     if (half == 0 && split == 0) a.delta[at * a.heads + head] = delta;
+    const float scale = BF ? a.scale : a.scale * __builtin_amdgcn_exp2f(-lift);
     if (a.key_splits > 1) {
         float* p = a.part_q + ((split * a.tokens_q + at) * a.heads + head) * a.dim;
 #pragma unroll
@@ -197,8 +232,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
                 const int d = 32 * b + 2 * i + 4 * half;
                 if (d < a.dim)
                     *reinterpret_cast<float4*>(p + d) =
-                        make_float4(acc[b][i] * a.scale, acc[b][i + 1] * a.scale,
-                                    acc[b][i + 2] * a.scale, acc[b][i + 3] * a.scale);
+                        make_float4(acc[b][i] * scale, acc[b][i + 1] * scale,
+                                    acc[b][i + 2] * scale, acc[b][i + 3] * scale);
             }
         return;
     }
@@ -210,8 +245,8 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
             const int d = 32 * b + 2 * i + 4 * half;
             if (d < a.dim)
                 *reinterpret_cast<uintx2*>(out + 2 * d) =
-                    uintx2{pack16<BF>(acc[b][i] * a.scale, acc[b][i + 1] * a.scale),
-                           pack16<BF>(acc[b][i + 2] * a.scale, acc[b][i + 3] * a.scale)};
+                    uintx2{pack16<BF>(acc[b][i] * scale, acc[b][i + 1] * scale),
+                           pack16<BF>(acc[b][i + 2] * scale, acc[b][i + 3] * scale)};
         }
 }
 
@@ -324,6 +359,7 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
 
+    float lift = kLiftSlope - kLiftP, up = __builtin_amdgcn_exp2f(lift);  // (fp16; of this lane's key)
     auto product = [&](const uintx4* x) {            // x kv^T, 32 rows x 32 keys
         floatx16 y;
 #pragma unroll
@@ -378,6 +414,10 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
             x[i + 2] = p4.z * (x[i + 2] - d4.z);
             x[i + 3] = p4.w * (x[i + 3] - d4.w);
         }
+        if constexpr (!BF) {
+            x *= up;
+            if (keep_in_range(x, acc, lift)) up = __builtin_amdgcn_exp2f(lift);
+        }
         add(qt, x);
     };
     // Iteration i0: tile i0 for the first waves (there is none past the end),
@@ -420,7 +460,8 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
         }
     }
     if (k0 + pair * 32 + (lane & 31) >= s.m) return;
-    const float scale = second ? a.scale : 1.f;
+    float scale = second ? a.scale : 1.f;
+    if constexpr (!BF) scale *= __builtin_amdgcn_exp2f(-kLiftP - (second ? lift : 0.f));
     if (a.row_splits > 1) {
         float* p = a.part_kv + (((split * 2 + (second ? 1 : 0)) * a.tokens_k + s.k0 + key) * a.kv_heads + kvh) * a.dim;
 #pragma unroll

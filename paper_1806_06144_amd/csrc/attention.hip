@@ -13,6 +13,9 @@
 // Scores, maximum, sum and output accumulate in float32. The probabilities
 // are rounded to 16 bits for the second product (at most 2^-8 of them in bf16,
 // as much as the output's own rounding); their sum is taken before that.
+// In fp16, whose bits thin out below 2^-14, they are 2^12 (2^14) and not 1 where
+// a row's largest score is: 131071 keys of 1.5 x 2^-24 beside one of 1 gave 0.0077
+// of V instead of 0.0114.
 //
 // What bounds it: many rows, the matrix units and the device's power (2 x 8192
 // tokens, 32 heads over 8, dim 128, causal, bf16: 1.09 ms, 1.01 PFLOP/s, where
@@ -131,6 +134,10 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     constexpr int kQuads = tile_quads(DP);
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
+    // Probabilities, before their division, are up to 2^(kLift + kRise) and
+    // for the largest score at least 2^kLift.
+    constexpr float kLift = BF ? 0.f : 12.f;
+    constexpr float kRise = BF ? 8.f : 3.f;
     // (arrays of their own: what is loaded into one is not waited for where
     // another is read)
     __shared__ uintx4 kt0[kKeys * kQuads];
@@ -219,10 +226,10 @@ __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[b][i]);
-            mx = pair_max(mx) * a.scale_log2;
+            mx = pair_max(mx) * a.scale_log2 - kLift;
             // The sums are brought to a new maximum only where it has risen
-            // by more than 8: probabilities up to 2^8 lose nothing.
-            if (__any(mx > top + 8.f)) {
+            // by more than kRise.
+            if (__any(mx > top + kRise)) {
                 const float now = fmaxf(top, mx);
                 const float shrink = __builtin_amdgcn_exp2f(top - now);
                 top = now;
@@ -303,6 +310,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
     constexpr int kSteps = DP / 16;
     constexpr int kBlocks = DP / 32;
     constexpr int kLoads = kWaveKeys * kQuads / 64;  // of K, and of V
+    constexpr float kLift = BF ? 0.f : 14.f;         // (probabilities up to 2^kLift)
     __shared__ uintx4 tiles_lds[4][2][kWaveKeys * kQuads];
     __shared__ float s_top[4][32], s_sum[4][32];
 
@@ -437,7 +445,7 @@ __global__ void __launch_bounds__(256, 2) attn_few_kernel(AttnArgs a) {
         float mx = sc[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sc[i]);
-        mx = pair_max(mx) * a.scale_log2;
+        mx = pair_max(mx) * a.scale_log2 - kLift;
         const float now = fmaxf(top, mx);
         const float shrink = __builtin_amdgcn_exp2f(top - now);
         top = now;

@@ -93,3 +93,33 @@ def test_fp16_slopes_past_the_range():
                         (grads[2], want[2], (g[:, 0].double().abs().sum(0) / m / scale)[None])):
         room = 1.1 * 2.0 ** -11 * (scale * terms + w.abs()) + 2.0 ** -25
         assert x.isfinite().all() and ((x[:, 0].double() - w).abs() <= room).all()
+
+
+@pytest.mark.parametrize("n,g,terms", [(1, 1, 512), (200, 1, 512), (1, 2048, 16384), (40, 512, 65536)])
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+def test_many_small_probabilities_beside_a_large_one(kind, n, g, terms):
+    """One key's probability 1, before the division, and 131071 of 1.5 x 2^-24
+    beside it, together 0.0117: below what fp16 holds with any accuracy. Keys
+    cut over workgroups or, where there are many heads (all of them alike, by
+    a stride of 0), not; terms: that a lane adds at most."""
+    import torch
+    import paper_1806_06144_amd as ep
+    from oracle.attention import U
+    dt = torch.float16 if kind == "fp16" else torch.bfloat16
+    m, d = 131072, 64
+    q = torch.zeros((n, g, d), dtype=dt, device="cuda")
+    q[:, :, 0] = 16.0                                # scores 16 k[0]: 0, and -16.25
+    k, v = (torch.zeros((m, 1, d), dtype=dt, device="cuda") for _ in range(2))
+    k[1:, 0, 0] = -1.015625
+    v[1:] = 1.0
+    k, v = (x.expand(-1, g, -1) for x in (k, v))
+    s, t = (torch.tensor([0, x], dtype=torch.int32, device="cuda") for x in (n, m))
+    out, lse = torch.empty_like(q), torch.empty((n, g), device="cuda")
+    ep.ep_attention(q, k, v, out, lse, s, t, 1.0, False)
+    rest = (m - 1) * np.exp(-16.25)
+    want = rest / (1 + rest)
+    # all probabilities are rounded alike (relative u), then the result; each of a lane's terms
+    # costs its float32 sum a step beside the large one, and exp2 some (an exponent of 23.4)
+    room = (terms + 64) * 2.0 ** -23
+    assert (out.double() - want).abs().max().item() <= want * (2 * U[kind] + room)
+    assert (lse.double() - np.log1p(rest)).abs().max().item() <= 4e-6 + room

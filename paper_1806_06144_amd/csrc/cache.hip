@@ -93,7 +93,9 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheArgs a) {
         const int b = seq_of(a.start, a.batch, t);
         if (b < 0) continue;
         // the new tokens are the sequence's last
-        const int64_t j = (int64_t)a.lengths[b] - a.start[b + 1] + t;
+        int first, count;
+        held_range(a.start[b], a.start[b + 1], (int)a.tokens, first, count);
+        const int64_t j = (int64_t)a.lengths[b] - (first + count) + t;
         int page = -1;
         if (j >= 0 && j < a.cols << a.page_shift)
             page = page_of(a.table, a.cols, b, a.pages, a.page_shift, j);
@@ -134,9 +136,9 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a) {
         const int t = (int)(i / chunks), h = (int)(i % chunks) * HEADS;
         const int b = seq_of(a.start, a.batch, t);
         if (b < 0) continue;
-        const int64_t j = (int64_t)t - a.start[b];
+        const int j = t - clamp_i(a.start[b], 0, (int)a.tokens);
         int page = -1;
-        if (j < a.lengths[b] && j < a.cols << a.page_shift)
+        if (j < a.lengths[b] && (int64_t)j < a.cols << a.page_shift)
             page = page_of(a.table, a.cols, b, a.pages, a.page_shift, j);
         if (page < 0) {
             if (a.err) *a.err = 1;

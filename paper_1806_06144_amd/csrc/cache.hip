@@ -137,13 +137,10 @@ __global__ void __launch_bounds__(256) cache_read_kernel(CacheArgs a) {
         const int b = seq_of(a.start, a.batch, t);
         if (b < 0) continue;
         const int j = t - clamp_i(a.start[b], 0, (int)a.tokens);
-        int page = -1;
-        if (j < a.lengths[b] && (int64_t)j < a.cols << a.page_shift)
-            page = page_of(a.table, a.cols, b, a.pages, a.page_shift, j);
-        if (page < 0) {
-            if (a.err) *a.err = 1;
-            continue;
-        }
+        const int length = a.lengths[b], held = held_length(length, a.cols, a.page_shift);
+        const int page = j < held ? page_of(a.table, a.cols, b, a.pages, a.page_shift, j) : -1;
+        if ((page < 0 || length != held) && a.err) *a.err = 1;
+        if (page < 0) continue;
         const int64_t from = page_slot(page, a.page_shift, j) * a.kv_heads + h;
         typedef std::conditional_t<E4M3, uintx2, uintx4> Quad;
         Quad k[HEADS], v[HEADS];

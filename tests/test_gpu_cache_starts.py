@@ -25,3 +25,19 @@ def test_starts_outside_the_rows_are_the_nearest_inside(eight):
         assert c.err.item() == 0
         got.append([x.view(torch.uint8) for x in (c.k, c.v, *back)])
     assert all(torch.equal(a, b) for other in got[1:] for a, b in zip(got[0], other))
+
+
+def test_lengths_past_the_table_are_reported():
+    import torch
+    rng = np.random.default_rng(3)
+    c = Cache(rng, "fp16", False, 2, 64, 16, [48, 48])
+    k, v = (rounded(rng, (96, 2, 64), "fp16").cuda() for _ in range(2))
+    c.write(k, v, [48, 48], [48, 48])
+    for length in (49, 2 ** 31 - 1):
+        c.err.zero_()
+        back = [torch.full((20, 2, 64), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+        c.ep.ep_cache_read(c.c, *back, c.table, c.ints([length, 48]), c.ints([0, 8, 20]), c.err)
+        assert c.err.item() == 1 and torch.equal(back[0][8:], k[48:60])
+    c.err.zero_()
+    c.ep.ep_cache_read(c.c, *back, c.table, c.ints([48, 48]), c.ints([0, 8, 20]), c.err)
+    assert c.err.item() == 0

@@ -396,8 +396,8 @@ int ep_device_probe(double* mfma_f32_tflops, double* shader_clock_mhz);
  */
 
 /* Rows of heads: element (t, h, c) at data[t row + h head + c], 16-bit.
- * data is 16-byte aligned, row and head are multiples of 8, at least 0 (of an
- * output at least dim: its rows must not overlap), row below 2^24. They may be
+ * data is 16-byte aligned, row and head are multiples of 8, at least 0, row
+ * below 2^24. Rows of an output must not overlap (EP_EINVAL). They may be
  * strides into a wider array; that of an axis of one element is not used. */
 typedef struct ep_rows {
     void* data;

@@ -50,6 +50,22 @@ int check_attn(const ep_attn* a, bool packed_keys) {
     return EP_OK;
 }
 
+// Whether rows of dim elements meet, where neither axis' stride is below dim:
+// token t of head i + h and token t + s of head i, s row within dim of h head.
+// Strides of which one spans the whole other axis are apart at a glance.
+bool rows_meet(const ep_rows& r, int64_t tokens, int64_t heads, int64_t dim) {
+    if (tokens == 1 || heads == 1) return false;
+    // (row < 2^24 and tokens < 2^30, so nothing here passes 64 bits)
+    if (r.head >= (tokens - 1) * r.row + dim) return false;
+    if (r.head <= r.row && r.row >= (heads - 1) * r.head + dim) return false;
+    for (int64_t h = 1; h < heads; ++h) {
+        const int64_t at = h * r.head, s = at / r.row;
+        if (s >= tokens) return false;
+        if ((s >= 1 && at - s * r.row < dim) || (s + 1 < tokens && (s + 1) * r.row - at < dim)) return true;
+    }
+    return false;
+}
+
 // (data may be NULL where there are no rows)
 // dim: of an output, whose rows must lie apart; 0: of an input.
 int check_rows(const char* name, const ep_rows& r, int64_t tokens, int64_t heads, int64_t dim) {
@@ -61,6 +77,9 @@ int check_rows(const char* name, const ep_rows& r, int64_t tokens, int64_t heads
             "%s: the rows' stride must be a multiple of 8 elements in [%d, 2^24)", name, (int)dim);
     REQUIRE(heads == 1 || (r.head % 8 == 0 && r.head >= dim),
             "%s: the heads' stride must be a multiple of 8 elements, at least %d", name, (int)dim);
+    REQUIRE(dim == 0 || !rows_meet(r, tokens, heads, dim),
+            "%s: its rows overlap: strides of %lld and %lld elements for %lld tokens of %lld heads",
+            name, (long long)r.row, (long long)r.head, (long long)tokens, (long long)heads);
     return EP_OK;
 }
 

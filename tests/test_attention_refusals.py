@@ -1,0 +1,49 @@
+"""More refusals of the attention calls, without a GPU."""
+
+import ctypes
+
+import pytest
+
+import paper_1806_06144_amd as ep
+from test_attention_host import A, _attn, _backward, _cache, _rows, _table
+
+
+def _forward(a, out):
+    """(with a bad address for work: what passes the checks of rows stops there)"""
+    return ep.raw_call("ep_attention", ctypes.byref(a), _rows(), _rows(), _rows(), out, A, A + 4,
+                       1 << 30, None)
+
+
+def _overlap(row, head, tokens, heads, dim):
+    """By the definition: does any pair of rows share an element?"""
+    at = sorted(t * row + h * head for t in range(tokens) for h in range(heads))
+    return any(b - a < dim for a, b in zip(at, at[1:]))
+
+
+LAYOUTS = [(64, 64), (512, 64), (64, 6400), (64, 448), (128, 192), (192, 128), (72, 64), (64, 72),
+           (520, 64), (504, 64), (64, 6336), (64, 6392), (128, 64), (256, 64), (320, 128),
+           (1 << 23, 64), (64, 1 << 40), (640, 192), (136, 408), (64, 1 << 62)]
+
+
+@pytest.mark.parametrize("row,head", LAYOUTS)
+@pytest.mark.parametrize("name,heads", [("out", 8), ("dq", 8), ("dk", 2), ("dv", 2), ("read", 2)])
+def test_outputs_whose_rows_overlap(name, heads, row, head):
+    """100 tokens of 8 heads, 2 key heads, of 64 elements."""
+    rows, cache, pages = _rows(row=row, head=head), _cache(), _table()
+    if name == "out":
+        rc = _forward(_attn(), rows)
+    elif name == "read":                             # (start, checked before v, is left out)
+        rc = ep.raw_call("ep_cache_read", ctypes.byref(cache), ctypes.byref(pages), ep.EP_BF16,
+                         rows, _rows(data=A + 2), 100, A, None)
+        name = "k"
+    else:
+        rc = _backward(_attn(), work=A + 4, **{name: rows})
+    assert rc == ep.EP_EINVAL
+    refused = ep.ep_last_error().startswith(name + ":")
+    assert refused == _overlap(row, head, 100, heads, 64), ep.ep_last_error()
+
+
+def test_one_token_or_one_head_needs_no_stride():
+    """The stride of an axis of one element is not looked at."""
+    for a, out in ((_attn(tokens_q=1), _rows(row=0)), (_attn(heads=1, kv_heads=1), _rows(head=0))):
+        assert _forward(a, out) == ep.EP_EINVAL and "work" in ep.ep_last_error()

@@ -407,7 +407,7 @@ typedef struct ep_rows {
 /* What the attention calls share. Bounds: 1 <= batch < 2^24; tokens_q,
  * tokens_k >= 0 and < 2^30; heads a multiple of kv_heads, with group = heads /
  * kv_heads: tokens_q group^2 < 2^32 and group <= 1024; kv_heads < 2^16; dim a
- * multiple of 8, 8 .. 128; scale > 0 and finite; 0 <= window < 2^30. */
+ * multiple of 8, 8 .. 128; scale > 0, scale log2(e) finite; 0 <= window < 2^30. */
 typedef struct ep_attn {
     int32_t type;               /* EP_BF16 or EP_FP16                          */
     int32_t causal;             /* 0 or 1                                      */

@@ -38,7 +38,8 @@ int check_attn(const ep_attn* a, bool packed_keys) {
                  attn_groups(a->kv_heads, a->tokens_k, kRowTile, a->batch) <= kMaxGroups / 2),
             "too many workgroups: kv_heads * (tokens_q * (heads / kv_heads) / 32 + batch) must be "
             "below 2^24, kv_heads * (tokens_k / 128 + batch) below 2^23");
-    REQUIRE(std::isfinite(a->scale) && a->scale > 0.f, "scale must be positive and finite");
+    REQUIRE(std::isfinite(a->scale * kLog2e) && a->scale > 0.f,
+            "scale must be positive, scale * log2(e) finite");
     REQUIRE(a->causal == 0 || a->causal == 1, "causal must be 0 or 1");
     REQUIRE(a->window >= 0 && a->window < kMaxTokens, "window must be in [0, 2^30)");
     REQUIRE(a->window == 0 || a->causal, "a window needs causal");

@@ -47,3 +47,12 @@ def test_one_token_or_one_head_needs_no_stride():
     """The stride of an axis of one element is not looked at."""
     for a, out in ((_attn(tokens_q=1), _rows(row=0)), (_attn(heads=1, kv_heads=1), _rows(head=0))):
         assert _forward(a, out) == ep.EP_EINVAL and "work" in ep.ep_last_error()
+
+
+def test_a_scale_that_overflows_in_units_of_log_2():
+    """scale log2(e) has to be finite as well."""
+    for scale, fine in ((2.3e38, True), (2.4e38, False), (3.4e38, False), (1e-45, True)):
+        a = _attn(scale=scale)
+        rc = ep.raw_call("ep_attention_bytes", ctypes.byref(a))
+        assert (rc >= 0) == fine
+        assert fine or "scale" in ep.ep_last_error()

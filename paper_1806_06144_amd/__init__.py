@@ -457,6 +457,8 @@ def _on_stream(device, stream, call):
         return call(_raw_stream(device.index), device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
+    elif stream is not None and stream.device != device:
+        raise ValueError(f"stream: expected one of {device}, got one of {stream.device}")
     with torch.cuda.device(device), torch.cuda.stream(stream):
         return call(torch.cuda.current_stream().cuda_stream, device)
 

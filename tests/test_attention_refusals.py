@@ -56,3 +56,18 @@ def test_a_scale_that_overflows_in_units_of_log_2():
         rc = ep.raw_call("ep_attention_bytes", ctypes.byref(a))
         assert (rc >= 0) == fine
         assert fine or "scale" in ep.ep_last_error()
+
+
+class _Stream:
+    def __init__(self, device):
+        self.device = device
+
+
+def test_a_stream_of_another_device():
+    """Work on one device's tensors does not go to another device's stream."""
+    import torch
+    called = []
+    with pytest.raises(ValueError, match="stream"):
+        ep._on_stream(torch.device("cuda", 0), _Stream(torch.device("cuda", 1)),
+                      lambda *a: called.append(a))
+    assert not called

@@ -446,7 +446,7 @@ def _attn(q, kv_heads, tokens_k, start_q, start_k, scale, causal, window, device
                   kv_heads, dim, tokens_q, tokens_k, window,
                   _dense(start_q, "start_q", _int32, starts, device),
                   None if start_k is None else _dense(start_k, "start_k", _int32, starts, device),
-                  dim ** -0.5 if scale is None else scale)
+                  max(dim, 1) ** -0.5 if scale is None else scale)
 
 
 def _on_stream(device, stream, call):

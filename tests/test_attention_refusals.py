@@ -71,3 +71,11 @@ def test_a_stream_of_another_device():
         ep._on_stream(torch.device("cuda", 0), _Stream(torch.device("cuda", 1)),
                       lambda *a: called.append(a))
     assert not called
+
+
+def test_rows_of_no_elements():
+    """dim = 0 has no scale of its own; it is refused like any other bad dim."""
+    import torch
+    q, s = torch.zeros((4, 2, 0), dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
+    a = ep._attn(q, 2, 4, s, s, None, True, 0, q.device)
+    assert ep.raw_call("ep_attention_bytes", ctypes.byref(a)) == ep.EP_EINVAL

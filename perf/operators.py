@@ -246,6 +246,7 @@ def prepare(case, seed):
     u = _inputs(case, seed)
     u["case"] = case
     u["scale"] = 1.0 / math.sqrt(case["dim"])
+    u["cached"] = sum(_lengths(case)[1])            # tokens, as a program that reads them back knows
     if case["op"] == "backward":                    # what the forward pass left
         u["out"], u["lse"] = _plain_forward(u)
     return u
@@ -409,7 +410,7 @@ def _own_run(st):
     cache = ep.EpCache(st["k_pages"], st["v_pages"], st["k_scale"], st["v_scale"])
     if case["op"] == "store":
         ep.ep_cache_write(cache, st["k"], st["v"], st["table"], st["lengths"], st["start_q"])
-        total = sum(_lengths(case)[1])
+        total = st["cached"]
         out = [torch.empty((total, case["kv_heads"], case["dim"]), dtype=st["k"].dtype,
                            device="cuda") for _ in range(2)]
         ep.ep_cache_read(cache, out[0], out[1], st["table"], st["lengths"], st["start_k"])

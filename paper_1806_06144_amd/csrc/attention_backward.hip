@@ -50,21 +50,21 @@ constexpr int kWaveRows = 8;          // of these, loaded by a wave
 constexpr int kStages = 4;            // tiles of rows in LDS (three are in use)
 constexpr int kKeyRange = 128;        // keys of a workgroup (dk, dv): 32 per wave
 
-constexpr float kLiftP = 14.f;        // fp16: exponents of the powers of two of p,
-constexpr float kLiftSlope = 60.f;    // and of ds where a row or key starts
+constexpr int kLiftP = 14;           // fp16: exponents of the powers of two of p,
+constexpr int kLiftSlope = 60;       // and of ds where a row or key starts
 
 // x: ds times 2^lift of a lane's row or key (which lanes l and l + 32 share),
 // acc its sums. Where one is past 2^15, brings them down to 2^11, which leaves
 // room to grow: 25 binades below hold all their bits.
 template <int BLOCKS>
-__device__ __forceinline__ bool keep_in_range(floatx16& x, floatx16 (&acc)[BLOCKS], float& lift) {
+__device__ __forceinline__ bool keep_in_range(floatx16& x, floatx16 (&acc)[BLOCKS], int& lift) {
     float most = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(x[i]));
     if (!__any(most > 0x1p15f)) return false;
     most = pair_max(most);
-    const float drop = most > 0x1p15f ? (float)(__builtin_amdgcn_frexp_expf(most) - 11) : 0.f;
-    const float by = __builtin_amdgcn_exp2f(-drop);
+    const int drop = most > 0x1p15f ? __builtin_amdgcn_frexp_expf(most) - 11 : 0;
+    const float by = __builtin_amdgcn_ldexpf(1.f, -drop);
     lift -= drop;
     x *= by;
 #pragma unroll
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     const bool mine = r0 + wave * 32 + (lane & 31) < s.rows;
     const float lse2 = a.lse[at * a.heads + head] * kLog2e;
     if (mine && half == 0 && split == 0) a.lse2[at * a.heads + head] = BF ? lse2 : lse2 - kLiftP;
-    float lift = BF ? 0.f : kLiftSlope;              // (of this lane's row)
+    int lift = BF ? 0 : kLiftSlope;                  // (of this lane's row)
 
     floatx16 acc[kBlocks];
 #pragma unroll
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
                 dp = mfma16<BF>(rd.rows(vt, 32 * b, i), gf[i], dp);
             }
             float p[16];
-            const float base = !BF && decltype(ds)::value ? lift - lse2 : -lse2;
+            const float base = !BF && decltype(ds)::value ? (float)lift - lse2 : -lse2;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale_log2, base));
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
     sweep(std::true_type{});
     if (!mine) return;
     if (half == 0 && split == 0) a.delta[at * a.heads + head] = delta;
-    const float scale = BF ? a.scale : a.scale * __builtin_amdgcn_exp2f(-lift);
+    const float scale = BF ? a.scale : __builtin_amdgcn_ldexpf(a.scale, -lift);
     if (a.key_splits > 1) {
         float* p = a.part_q + ((split * a.tokens_q + at) * a.heads + head) * a.dim;
 #pragma unroll
@@ -359,7 +359,8 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
 
-    float lift = kLiftSlope - kLiftP, up = __builtin_amdgcn_exp2f(lift);  // (fp16; of this lane's key)
+    int lift = kLiftSlope - kLiftP;                  // (fp16; of this lane's key)
+    float up = __builtin_amdgcn_ldexpf(1.f, lift);
     auto product = [&](const uintx4* x) {            // x kv^T, 32 rows x 32 keys
         floatx16 y;
 #pragma unroll
@@ -416,7 +417,7 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
         }
         if constexpr (!BF) {
             x *= up;
-            if (keep_in_range(x, acc, lift)) up = __builtin_amdgcn_exp2f(lift);
+            if (keep_in_range(x, acc, lift)) up = __builtin_amdgcn_ldexpf(1.f, lift);
         }
         add(qt, x);
     };
@@ -461,7 +462,7 @@ __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArg
     }
     if (k0 + pair * 32 + (lane & 31) >= s.m) return;
     float scale = second ? a.scale : 1.f;
-    if constexpr (!BF) scale *= __builtin_amdgcn_exp2f(-kLiftP - (second ? lift : 0.f));
+    if constexpr (!BF) scale = __builtin_amdgcn_ldexpf(scale, -kLiftP - (second ? lift : 0));
     if (a.row_splits > 1) {
         float* p = a.part_kv + (((split * 2 + (second ? 1 : 0)) * a.tokens_k + s.k0 + key) * a.kv_heads + kvh) * a.dim;
 #pragma unroll

@@ -188,8 +188,9 @@ def _torch():
 
 
 _int32, _float32 = _torch().int32, _torch().float32
-_current_device = _torch()._C._cuda_getDevice
-_raw_stream = _torch()._C._cuda_getCurrentRawStream
+# (a torch without devices has neither; what needs no tensors works there too)
+_current_device = getattr(_torch()._C, "_cuda_getDevice", None)
+_raw_stream = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)
 _ATTN_TYPES = {_torch().bfloat16: EP_BF16, _torch().float16: EP_FP16}
 _CACHE_TYPES = {**_ATTN_TYPES, _torch().float8_e4m3fn: EP_E4M3, _torch().uint8: EP_E4M3}
 

@@ -1,6 +1,9 @@
 """More refusals of the attention calls, without a GPU."""
 
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -79,3 +82,18 @@ def test_rows_of_no_elements():
     q, s = torch.zeros((4, 2, 0), dtype=torch.bfloat16), torch.tensor([0, 4], dtype=torch.int32)
     a = ep._attn(q, 2, 4, s, s, None, True, 0, q.device)
     assert ep.raw_call("ep_attention_bytes", ctypes.byref(a)) == ep.EP_EINVAL
+
+
+def test_the_binding_loads_beside_a_torch_without_devices():
+    """As it did before it had attention."""
+    program = """
+import torch
+for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+import paper_1806_06144_amd as ep
+print(ep.raw_call("ep_sync", None) == ep.EP_EINVAL)
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", program], cwd=root, capture_output=True, text=True)
+    assert r.stdout == "True\n", r.stderr

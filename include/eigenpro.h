@@ -385,8 +385,9 @@ int ep_device_probe(double* mfma_f32_tflops, double* shader_clock_mhz);
  * Mask. Query i of a sequence of n queries and m keys stands at position
  * p = i + m - n. With causal it sees keys j <= p, with a window w > 0 (causal
  * only) those with j > p - w; else it sees all. A query that sees nothing (p
- * < 0, no keys) gets out = 0, lse = -infinity and no gradient. Keys and
- * values must be finite: one that is not may reach any query of its sequence.
+ * < 0, no keys) gets out = 0, lse = -infinity and no gradient. Rows must be
+ * finite: a key or value that is not may reach any query of its sequence, and a
+ * query or a dout any key's gradient.
  *
  * Arithmetic. Scores, softmax statistics and sums are float32; probabilities
  * (and, for gradients, p (dp - D)) are rounded to the element type for their
@@ -406,7 +407,9 @@ typedef struct ep_rows {
 
 /* What the attention calls share. Bounds: 1 <= batch < 2^24; tokens_q,
  * tokens_k >= 0 and < 2^30; heads a multiple of kv_heads, with group = heads /
- * kv_heads: tokens_q group^2 < 2^32 and group <= 1024; kv_heads < 2^16; dim a
+ * kv_heads: tokens_q group < 2^30, tokens_q group^2 < 2^32 and group <= 1024;
+ * kv_heads < 2^16; kv_heads (tokens_q group / 32 + batch) < 2^24 and kv_heads
+ * (tokens_k / 128 + batch) < 2^23 (not ep_cache_attention); dim a
  * multiple of 8, 8 .. 128; scale > 0, scale log2(e) finite; 0 <= window < 2^30. */
 typedef struct ep_attn {
     int32_t type;               /* EP_BF16 or EP_FP16                          */
@@ -502,8 +505,9 @@ typedef struct ep_pages {
  *   type    of k and v, EP_BF16 or EP_FP16 (that of the cache unless EP_E4M3).
  *   k, v    tokens x kv_heads x dim.   start  device, batch + 1.
  * Tokens without a place (a bad page, a position below 0 or past the table)
- * are not written and set *err. A page that two sequences share gets either's
- * values where both write the same slot.
+ * are not written and set *err. Where two new tokens share a slot (sequences
+ * that share a page), it gets pieces of either, and an EP_E4M3 row
+ * possibly one's values with the other's scale: write a shared slot once.
  * Errors: EP_EINVAL, EP_EDEVICE.
  */
 int ep_cache_write(const ep_cache* c, const ep_pages* p, int type, ep_rows k, ep_rows v,

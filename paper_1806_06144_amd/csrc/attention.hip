@@ -17,12 +17,13 @@
 // a row's largest score is: 131071 keys of 1.5 x 2^-24 beside one of 1 gave 0.0077
 // of V instead of 0.0114.
 //
-// What bounds it: many rows, the matrix units and the device's power (2 x 8192
-// tokens, 32 heads over 8, dim 128, causal, bf16: 1.09 ms, 1.01 PFLOP/s, where
-// a library product of 8192^3 reaches 1.15); at dim 64 the softmax's vector
-// work (24 ragged sequences of up to 1000, 16 heads: 78 us, 0.55 PFLOP/s); few
-// rows, memory (64 single tokens over up to 16000: 415 us, 5.6 TB/s; e4m3 rows
-// of up to 100000 tokens: 222 us, 4.3 TB/s).
+// What bounds it: many rows, products and softmax together: matrix units are
+// busy 48 % of the cycles, vector units 45 % (2 x 8192 tokens, 32 heads over 8,
+// dim 128, causal, bf16: 1.10 ms, 1.00 PFLOP/s, where a library product of 8192^3
+// reaches 1.12); at dim 64 the softmax's vector work (58 %, products 28 %; 24
+// ragged sequences of up to 1000, 16 heads: 78 us, 0.55 PFLOP/s); few rows,
+// memory (64 single tokens over up to 16000: 414 us, 5.6 TB/s; e4m3 rows of up
+// to 100000 tokens: 225 us, 4.2 TB/s).
 #include "attn.h"
 #include "ep_internal.h"
 #include "launch.h"
@@ -126,9 +127,9 @@ struct KeyTiles {
 
 // Tiles go straight into LDS a tile ahead: 2118 us at 2 x 8192 tokens when they
 // went through registers between two barriers, 1119 like this. Two workgroups
-// a CU (64 KB of LDS, 200 registers) overlap one's products with the other's
-// softmax; forming the next tile's scores during this one's softmax instead
-// took 1128 us against 1090.
+// a CU (64 KB of LDS; at dim 128 218 to 228 registers, up to 256 with e4m3
+// pages) overlap one's products with the other's softmax; forming the next
+// tile's scores during this one's softmax instead took 1128 us against 1090.
 template <bool BF, int DP, int SOURCE>
 __global__ void __launch_bounds__(256, 2) attn_kernel(AttnArgs a) {
     constexpr int kQuads = tile_quads(DP);

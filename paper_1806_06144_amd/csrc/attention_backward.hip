@@ -5,11 +5,12 @@
 //   dv_j = sum_i p_ij dout_i,
 // the sums over i running over the heads of a group too.
 //
-// What bounds them: the matrix units and the device's power (2 x 4096 tokens, 32
-// heads over 8, dim 128, bf16: 420 us for dq and 670 for dk and dv, 0.92
-// PFLOP/s of the seven products), at dim 64 and short ranges vector work and
-// barriers (12 ragged sequences of up to 2047 with a window of 512, 12 heads:
-// 79 and 100 us).
+// What bounds them (matrix units' busy cycles, waves' waiting ones): 2 x 4096
+// tokens, 32 heads over 8, dim 128, bf16: at least 412 us for dq (49 %, 37 %) and
+// 664 for dk and dv (39 %, 34 %), 1036 one after another, 0.93 PFLOP/s of the
+// seven products; at dim 64 with short ranges barriers and vector work (12
+// ragged sequences of up to 2047 with a window of 512, 12 heads, fp16: 81 us
+// (23 %, 37 %) and 102 (23 %, 39 %)).
 //
 // Two kernels, each owning what it sums, so there are no atomics and the
 // results do not depend on the order of the workgroups: dq walks the keys as
@@ -42,8 +43,11 @@ constexpr int kKeyTile = 64;          // keys of a tile (dq)
 constexpr int kWaveKeys = 16;         // of these, loaded by a wave
 // D_i = out_i.dout_i carries the rounding of out, which beside ds counts as
 // 1 / sqrt(keys): rows of at most this many keys sum p_ij dp_ij in a sweep of
-// their own instead (three sequences of 201 in bf16: dq 1.42 times as far off
-// as the exact one rounded, against 1.50).
+// their own instead. 12 sequences of 201 (256, 512) in bf16, 12 heads of 64, dq's
+// error beside that of the exact one rounded: without 1.49 (1.57, 1.48) in 32 (35,
+// 57) us, up to 256 keys 1.40 (1.44, 1.41) in 37 (39, 61), up to 512 keys 1.40
+// (1.44, 1.40) in 37 (39, 68), where the second sweep gains nothing any more. (Up
+// to 128 keys: 1.41 (1.45, 1.41) in 33 (35, 58).)
 constexpr int kSummedKeys = 256;
 constexpr int kStepRows = 32;         // rows of a tile (dk, dv)
 constexpr int kWaveRows = 8;          // of these, loaded by a wave
@@ -255,11 +259,10 @@ __global__ void __launch_bounds__(256, 2) attn_dq_kernel(AttnArgs a) {
 // and dk^T += Q^T dS, a tile of rows behind. Each holds its operand of K or V
 // (32 registers at dim 128) and one sum (64), which leaves room for two waves
 // a SIMD, one of each kind, whose matrix products, exponentials and LDS reads
-// overlap. One wave with both sums (192 registers) either ran alone on its
-// SIMD, waiting for X at 2 x 4096 tokens,
-// 32 heads over 8, dim 128, where this takes DKVTIME. Products whose result has a key
-// a lane (16 rows of ONE key) leave P and dS in the order in which the second
-// products take them.
+// overlap. One wave with both operands and sums (192 registers) ran alone on its
+// SIMD: 880 us at 2 x 4096 tokens, 32 heads over 8, dim 128, where pairs took 690
+// with all else the same. Products whose result has a key a lane (16 rows of ONE
+// key) leave P and dS in the order in which the second products take them.
 template <bool BF, int DP>
 __global__ void __launch_bounds__(512, DP == 64 ? 4 : 2) attn_dkv_kernel(AttnArgs a) {
     constexpr int kQuads = tile_quads(DP);
@@ -550,7 +553,9 @@ void launch(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 // Cuts of the rows, where ranges of 128 keys alone leave the device's 256
-// workgroups idle: at least 4 tiles of rows each.
+// workgroups idle: at least 4 tiles of rows each (all gradients, 8 heads of 128,
+// 512 rows over 64 keys: 31 us uncut, 23.2 like this, 22.6 from 2 tiles on, 26.5
+// from 8; 32 heads over 8, 256 rows and keys: 60, 44, 47, 44).
 int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads) {
     const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_k), 1);
     const int64_t groups = kv_heads * std::max(sequences, ceil_div(tokens_k, kKeyRange));
@@ -561,7 +566,9 @@ int attn_row_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t h
 }
 
 // Cuts of the keys, where tiles of 128 rows alone leave its 512 slots idle: at
-// least 512 keys each.
+// least 512 keys each (all gradients, 8 heads of 128, 64 rows over 4096 keys: 126
+// us uncut, 38 like this, 34 from 256 keys on, 51 from 1024; 512 rows over 8192
+// keys: 283, 100, 98, 102).
 int attn_key_splits(int64_t batch, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads) {
     const int64_t sequences = std::max<int64_t>(std::min(batch, tokens_q), 1);
     const int64_t rows = tokens_q * (heads / kv_heads);

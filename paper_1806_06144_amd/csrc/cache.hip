@@ -17,7 +17,7 @@
 // Both kernels are bound by memory: a row is held by a group of 16 (8 for
 // dim <= 64) lanes, 16 bytes a lane, and a group takes up to four heads at once.
 // e4m3 pages of 8 heads of 128: 9087 tokens in 17 us (3.3 TB/s), 40647 back in
-// 42 (6.0 TB/s; 61 a head at a time).
+// 43 (5.9 TB/s; 61 a head at a time).
 #include "attn.h"
 #include "ep_internal.h"
 #include "launch.h"
